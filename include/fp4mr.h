@@ -72,7 +72,8 @@ enum {
     FP4MR_A_SCALE43 = 1u << 8,            /* MXFP4 products: the A operand was quantized with SCALE_ROUND43   */
     FP4MR_W_SCALE43 = 1u << 9,            /* MXFP4 products: the W operand was quantized with SCALE_ROUND43   */
     FP4MR_SCALE_FIT_TENSOR = 1u << 10,    /* NVFP4 quantize ops, with SCALE_MSE: also fit the tensor scale    */
-    FP4MR_SCALE_FIT_RANGE = 1u << 11      /* MXFP4 quantize ops: scale byte fitted to the tensor's range (below) */
+    FP4MR_SCALE_FIT_RANGE = 1u << 11,     /* MXFP4 quantize ops: scale byte fitted to the tensor's range (below) */
+    FP4MR_SILU_MUL = 1u << 12             /* fp8_quantize: quantize silu(gate) * up of rows [gate | up]       */
 };
 
 /* operation selector for fp4_workspace_bytes */
@@ -355,6 +356,64 @@ fp4mr_status_t fp4_set_option(int option, int value);
  */
 enum { FP4MR_PROBE_MFMA_FP4 = 0, FP4MR_PROBE_MFMA_F16 = 1, FP4MR_PROBE_COPY = 2, FP4MR_PROBE_READ = 3 };
 fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* stream);
+
+/*
+ * 8-bit linear layers: E4M3 codes with one fp32 scale per block of 128, for the layers of a model that are kept at 8 bits beside the
+ * 4-bit ones.  An operand stands for  code * scale :
+ *   activations  codes [M,K] bytes, scales [M, K/128] floats: a scale per 128 columns of a row
+ *   weights      codes [N,K] bytes, scales [ceil(N/128), K/128] floats: a scale per 128 x 128 block (the last block of rows may be short);
+ *                of several experts [E,N,K] and [E, ceil(N/128), K/128]
+ * all row-major and contiguous.  A code is an E4M3 "fn" byte (bias 7, max 448, no infinities, NaN 0x7f and 0xff).  The quantizers write
+ *   scale = max(amax, 2^-100) / 448 ,  code = the E4M3 value nearest to  v * (448 / max(amax, 2^-100)) , ties to even ,
+ * with amax the block's largest |v| and every operation in binary32.  A block that holds a NaN or an infinity has a scale that is
+ * not finite, and every output of a product that reads it is NaN or infinite.
+ * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24.  No rows (M, or rows, of 0) is not an
+ * error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.
+ *
+ * fp8_rmsnorm_quantize: codes, scales = Q(v),  v = h * weight / sqrt(mean(h^2) + eps),  h = bf16(x + residual), or x.
+ *   x            bf16, rows of K elements x_stride elements apart (x_stride >= K, a multiple of 8)
+ *   residual     bf16 [M,K] or NULL;  residual_out (NULL without residual, else required) receives h, and may be residual, or x
+ *                where x_stride == K
+ *   weight       bf16 [K];  K <= 65536
+ *   norm_out     bf16 [M,K] or NULL: receives v rounded to bf16 (what a router reads)
+ * Outputs must not overlap inputs or each other other than as said.  eps >= 0, else FP4MR_ERR_SHAPE.
+ */
+fp4mr_status_t fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t M, int64_t K,
+                                    float eps, void* codes_out, float* scales_out, void* residual_out, void* norm_out,
+                                    uint32_t flags, void* stream);
+
+/*
+ * codes, scales = Q(x) of bf16 activations, or with FP4MR_SILU_MUL of  silu(gate) * up , where a row of x is [gate | up], 2K elements.
+ * Rows are x_stride elements apart (at least what a row holds, a multiple of 8).  No workspace.
+ */
+fp4mr_status_t fp8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t K, void* codes_out, float* scales_out, uint32_t flags,
+                            void* stream);
+
+/* codes, scales = Q(w) of the bf16 weights [experts, N, K] (experts = 1: one matrix), a scale per 128 x 128 block of each expert. */
+fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes_out, float* scales_out,
+                                    uint32_t flags, void* stream);
+
+/*
+ * out[M,N] = A W^T  from 8-bit operands: every 128 columns' products are summed by the matrix instruction and added in fp32 with their two
+ * scales.  out is bf16, or fp32 with FP4MR_OUT_F32.  For a bf16 output the 8-bit matrix instruction sums eight products at a time and drops what
+ * lies below 2^-13 of the largest of them: an output is within (2^-10 + K 2^-31 + 2^-16) sum |a w| of the exact product before its rounding.  For an fp32
+ * output the codes are multiplied as fp16 with fp32 sums, at less than half the rate: within (K / 128 + 129) 2^-24 sum |a w|.
+ */
+fp4mr_status_t fp8_gemm(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales, int64_t M, int64_t N,
+                        int64_t K, void* out, uint32_t flags, void* stream);
+
+/*
+ * The same with rows grouped by expert: rows offsets[e] .. offsets[e+1] - 1 of out are those rows of A times the weights of expert e.
+ *   a_codes, a_scales  activations of a_rows rows
+ *   offsets      device int32 [experts + 1], not decreasing, 0 .. rows (a number outside that range counts as the nearest within it); an
+ *                expert may have no rows.  Rows of out that no expert has are not written.
+ *   index        device int32 [rows], the row of A for each row of out (so that a token's row is read by each of its experts from one
+ *                place), or NULL: row t of A for row t of out, a_rows == rows.  A negative index, or one of a_rows or more, stands for a row of zeros.
+ * offsets and index need 4-byte alignment only.  rows and a_rows <= 2^24, experts <= 65536.
+ */
+fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int64_t a_rows, const void* w_codes, const float* w_scales,
+                                const int32_t* offsets, const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K,
+                                void* out, uint32_t flags, void* stream);
 
 /* Bytes of device scratch the given operation needs (0 = none).  rows = M for the quantize ops. */
 size_t fp4_workspace_bytes(int op, int64_t M, int64_t N, int64_t K, fp4mr_fmt_t fmt, uint32_t flags);

@@ -32,6 +32,7 @@ SCALE_ROUND43 = 1 << 7
 SCALE_FIT_TENSOR = 1 << 10
 SCALE_FIT_RANGE = 1 << 11
 FIT_RANGE_FLOATS = 258
+SILU_MUL = 1 << 12
 A_SCALE43 = 1 << 8
 W_SCALE43 = 1 << 9
 OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC = 0, 1, 2
@@ -70,6 +71,16 @@ lib.fp4_probe.argtypes = [_i32, _p, _sz, _i32, _p]
 lib.fp4_probe.restype = _i32
 lib.fp4_dequantize.argtypes = [_p, _p, _p, _i64, _i64, _i32, _p, _u32, _p]
 lib.fp4_dequantize.restype = _i32
+lib.fp8_rmsnorm_quantize.argtypes = [_p, _i64, _p, _p, _i64, _i64, ctypes.c_float, _p, _p, _p, _p, _u32, _p]
+lib.fp8_rmsnorm_quantize.restype = _i32
+lib.fp8_quantize.argtypes = [_p, _i64, _i64, _i64, _p, _p, _u32, _p]
+lib.fp8_quantize.restype = _i32
+lib.fp8_quantize_weights.argtypes = [_p, _i64, _i64, _i64, _p, _p, _u32, _p]
+lib.fp8_quantize_weights.restype = _i32
+lib.fp8_gemm.argtypes = [_p, _p, _p, _p, _i64, _i64, _i64, _p, _u32, _p]
+lib.fp8_gemm.restype = _i32
+lib.fp8_grouped_gemm.argtypes = [_p, _p, _i64, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _p, _u32, _p]
+lib.fp8_grouped_gemm.restype = _i32
 lib.fp4_set_option.argtypes = [_i32, _i32]
 lib.fp4_set_option.restype = _i32
 
@@ -329,6 +340,117 @@ def fp4_probe(which: int, buf, iters: int = 1) -> None:
     """Launch one ceiling-measurement kernel on the current stream (see fp4_probe in the header); buf: cuda uint8 tensor."""
     assert buf.is_cuda and buf.is_contiguous()
     _check(lib.fp4_probe(int(which), buf.data_ptr(), buf.numel() * buf.element_size(), int(iters), _stream()))
+
+
+# ---- 8-bit linear layers: E4M3 codes (torch.float8_e4m3fn) with a float32 scale per 128 columns of a row (activations: codes [M,K],
+# scales [M, K/128]) or per 128 x 128 block (weights: codes [N,K], scales [ceil(N/128), K/128], or with experts in front)
+FP8_BLOCK = 128
+_E4M3 = torch.float8_e4m3fn
+
+
+def _rows(x):
+    """bf16 cuda [M, any] whose rows may be apart: (rows, elements of a row, elements between rows)."""
+    assert x.is_cuda and x.dim() == 2 and x.dtype == torch.bfloat16 and (x.stride(1) == 1 or x.shape[1] <= 1)
+    return x.shape[0], x.shape[1], x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _fp8_outputs(x, M: int, K: int, codes, scales):
+    empty = x.new_empty if type(x) is _Tensor else _plain_empty(x)
+    codes = empty((M, K), dtype=_E4M3) if codes is None else codes
+    scales = empty((M, K // FP8_BLOCK), dtype=torch.float32) if scales is None else scales
+    _is_operand(codes, scales, (M, K), (M, K // FP8_BLOCK))
+    return codes, scales
+
+
+def _is_operand(codes, scales, shape, scale_shape):
+    assert codes.is_cuda and codes.dtype == _E4M3 and codes.is_contiguous() and tuple(codes.shape) == shape
+    assert scales.is_cuda and scales.dtype == torch.float32 and scales.is_contiguous() and tuple(scales.shape) == scale_shape
+
+
+def _is_bf16(t, *shape):
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == shape
+
+
+def fp8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residual_out=None, norm_out=None, codes=None, scales=None):
+    """codes, scales, h = Q(v) with v = h * weight / sqrt(mean(h^2) + eps) and h = bf16(x + residual), or x (then the third result is None).
+    x: bf16 [M,K], rows may be apart (K % 128 == 0, K <= 65536); weight: bf16 [K]; residual: bf16 [M,K].  residual_out: where h goes (may be residual
+    or x themselves, a new tensor if None); norm_out: bf16 [M,K] to receive v too."""
+    M, K, stride = _rows(x)
+    _is_bf16(weight, K)
+    empty = x.new_empty if type(x) is _Tensor else _plain_empty(x)
+    if residual is not None:
+        _is_bf16(residual, M, K)
+        if residual_out is None:
+            residual_out = empty((M, K), dtype=torch.bfloat16)
+    if residual_out is not None:
+        _is_bf16(residual_out, M, K)
+    if norm_out is not None:
+        _is_bf16(norm_out, M, K)
+    codes, scales = _fp8_outputs(x, M, K, codes, scales)
+    _check(lib.fp8_rmsnorm_quantize(x.data_ptr(), stride, _ptr(residual), weight.data_ptr(), M, K, eps, codes.data_ptr(), scales.data_ptr(), _ptr(residual_out),
+                                    _ptr(norm_out), 0, _stream()))
+    return codes, scales, residual_out
+
+
+def fp8_quantize(x, *, flags: int = 0, codes=None, scales=None):
+    """codes, scales = Q(x) of bf16 activations [M,K], or with SILU_MUL of silu(x[:, :K]) * x[:, K:] of x [M, 2K]; rows may be apart, K % 128 == 0."""
+    M, K, stride = _rows(x)
+    if flags & SILU_MUL:
+        assert K % 2 == 0
+        K //= 2
+    codes, scales = _fp8_outputs(x, M, K, codes, scales)
+    _check(lib.fp8_quantize(x.data_ptr(), stride, M, K, codes.data_ptr(), scales.data_ptr(), flags, _stream()))
+    return codes, scales
+
+
+def fp8_quantize_weights(w, *, codes=None, scales=None):
+    """codes, scales = Q(w) of bf16 weights [N,K], or of experts [E,N,K]: a scale per 128 x 128 block."""
+    assert w.is_cuda and w.dim() in (2, 3) and w.dtype == torch.bfloat16 and w.is_contiguous()
+    N, K = w.shape[-2:]
+    shape = (*w.shape[:-2], -(-N // FP8_BLOCK), K // FP8_BLOCK)
+    empty = w.new_empty if type(w) is _Tensor else _plain_empty(w)
+    codes = empty(tuple(w.shape), dtype=_E4M3) if codes is None else codes
+    scales = empty(shape, dtype=torch.float32) if scales is None else scales
+    _is_operand(codes, scales, tuple(w.shape), shape)
+    _check(lib.fp8_quantize_weights(w.data_ptr(), w.shape[0] if w.dim() == 3 else 1, N, K, codes.data_ptr(), scales.data_ptr(), 0, _stream()))
+    return codes, scales
+
+
+def _product_out(a_codes, a_scales, w_codes, w_scales, dim: int, rows: int, flags: int, out):
+    assert a_codes.dim() == 2 and w_codes.dim() == dim
+    N, K = w_codes.shape[-2:]
+    _is_operand(a_codes, a_scales, (a_codes.shape[0], K), (a_codes.shape[0], K // FP8_BLOCK))
+    _is_operand(w_codes, w_scales, tuple(w_codes.shape), (*w_codes.shape[:-2], -(-N // FP8_BLOCK), K // FP8_BLOCK))
+    dtype = torch.float32 if flags & OUT_F32 else torch.bfloat16
+    if out is None:
+        empty = a_codes.new_empty if type(a_codes) is _Tensor else _plain_empty(a_codes)
+        out = empty((rows, N), dtype=dtype)
+    assert out.is_cuda and out.dtype == dtype and out.is_contiguous() and tuple(out.shape) == (rows, N)
+    return out, N, K
+
+
+def fp8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None):
+    """out[M,N] = A W^T (bf16, or fp32 with OUT_F32) from the codes and scales of activations [M,K] and weights [N,K]."""
+    M = a_codes.shape[0]
+    out, N, K = _product_out(a_codes, a_scales, w_codes, w_scales, 2, M, flags, out)
+    _check(lib.fp8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, out.data_ptr(), flags, _stream()))
+    return out
+
+
+def fp8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=None, flags: int = 0, out=None):
+    """Rows offsets[e] .. offsets[e+1] - 1 of out = those rows of A times the weights of expert e, w_codes [E,N,K]; offsets: int32 cuda [E+1].
+    rows: int32 cuda [T], the row of A for each row of out (outside A: a row of zeros); without it out has A's rows.  Rows of out that no expert has are
+    not written (a new out holds what its memory held)."""
+    E = w_codes.shape[0]
+    assert offsets.is_cuda and offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.numel() == E + 1
+    T = a_codes.shape[0]
+    if rows is not None:
+        assert rows.is_cuda and rows.dtype == torch.int32 and rows.dim() == 1 and rows.is_contiguous()
+        T = rows.shape[0]
+    out, N, K = _product_out(a_codes, a_scales, w_codes, w_scales, 3, T, flags, out)
+    _check(lib.fp8_grouped_gemm(a_codes.data_ptr(), a_scales.data_ptr(), a_codes.shape[0], w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), _ptr(rows),
+                                T, E, N, K, out.data_ptr(), flags, _stream()))
+    return out
 
 
 def set_option(option: int, value: int) -> None:

@@ -1,0 +1,241 @@
+// Operands of the 8-bit linear layers: E4M3 codes with one fp32 scale per 128 columns of a row (activations) or per 128 x 128 block
+// (weights), behind the root-mean-square norm, behind silu(gate) * up, or of a tensor as it is.
+//
+//   s = max(amax, 2^-100) / 448,   code = e4m3(v * (448 / max(amax, 2^-100)))          amax: the block's largest |v|
+//
+// v is held in fp32 from the bf16 input to the code, which is the only rounding to fewer bits (but for the bf16 copies that a caller
+// asks for).  2^-100 keeps the reciprocal finite and gives a block of zeros the code 0 and a finite scale.  amax is an integer maximum
+// of the magnitudes' bit patterns, which orders infinity above every number and NaN above that: a block that holds one has the scale
+// infinity or NaN, and every product with it is NaN.
+#include "device_util.hpp"
+#include "internal.hpp"
+
+namespace fp4mr {
+namespace {
+
+constexpr float kE4m3Max = 448.0f;
+constexpr uint32_t kAmaxLeast = 27u << 23;   // 2^-100
+
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ void load8(const __bf16* p, float (&v)[8])
+{
+    const v8b t = __builtin_bit_cast(v8b, *reinterpret_cast<const v4i*>(p));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+}
+
+__device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
+{
+    v8b t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (__bf16)v[i];
+    *reinterpret_cast<v4i*>(p) = __builtin_bit_cast(v4i, t);
+}
+
+__device__ __forceinline__ uint32_t amax8(const float (&v)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+
+// Largest value among the sixteen lanes that hold a block of 128, in all of them.
+__device__ __forceinline__ uint32_t max16(uint32_t m)
+{
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));    // quad_perm [1,0,3,2]
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true));    // quad_perm [2,3,0,1]
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x124, 0xf, 0xf, true));   // row_ror 4
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x128, 0xf, 0xf, true));   // row_ror 8
+    return m;
+}
+
+__device__ __forceinline__ v2i codes8(const float (&v)[8], float inv)
+{
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, lo, true);
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
+    return v2i{lo, hi};
+}
+
+// Codes of a lane's eight values of a block, and the block's scale from its first lane.
+__device__ __forceinline__ void quantize8(const float (&v)[8], uint8_t* codes, float* scale, int lane)
+{
+    const float amax = __uint_as_float(max(max16(amax8(v)), kAmaxLeast));
+    *reinterpret_cast<v2i*>(codes) = codes8(v, kE4m3Max / amax);
+    if ((lane & 15) == 0) *scale = amax / kE4m3Max;
+}
+
+// silu(gate) * up
+__device__ __forceinline__ float silu_mul(float g, float u)
+{
+    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
+}
+
+struct QuantArgs {
+    const __bf16* x;
+    int64_t x_stride, rows, K;
+    uint8_t* codes;
+    float* scales;
+};
+
+// Sixteen lanes to a block of 128, in the order of the outputs.
+template <bool SILU>
+__global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantArgs a)
+{
+    const int64_t per_row = a.K / 8, total = a.rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per_row, col = (i - row * per_row) * 8;
+        const __bf16* x = a.x + row * a.x_stride + col;
+        float v[8];
+        load8(x, v);
+        if constexpr (SILU) {
+            float u[8];
+            load8(x + a.K, u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = silu_mul(v[j], u[j]);
+        }
+        quantize8(v, a.codes + i * 8, a.scales + i / 16, threadIdx.x);
+    }
+}
+
+struct NormArgs {
+    const __bf16* x;
+    const __bf16* residual;       // or null
+    const __bf16* weight;
+    __bf16* residual_out;
+    __bf16* norm_out;             // or null
+    uint8_t* codes;
+    float* scales;
+    int64_t x_stride, rows;
+    int K;
+    float eps;
+};
+
+// A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes.
+template <int T, int CH>
+__global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
+{
+    __shared__ float part[T / 64];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float v[CH][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * T + (int)threadIdx.x) * 8;
+        if (col < a.K) {
+            load8(a.x + row * a.x_stride + col, v[c]);
+            if (a.residual) {
+                float r[8];
+                load8(a.residual + row * a.K + col, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = (float)(__bf16)(v[c][i] + r[i]);   // the stream that is kept is the one that is normed
+                store8(a.residual_out + row * a.K + col, v[c]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    if constexpr (T > 64) {
+        if (lane == 0) part[wave] = sum;
+        __syncthreads();
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T / 64; ++i) sum += part[i];
+    }
+    const float rstd = 1.0f / sqrtf(sum / (float)a.K + a.eps);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * T + (int)threadIdx.x) * 8;
+        if (col < a.K) {   // (whole blocks of sixteen lanes)
+            float w[8];
+            load8(a.weight + col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[i];
+            if (a.norm_out) store8(a.norm_out + row * a.K + col, v[c]);
+            quantize8(v[c], a.codes + row * a.K + col, a.scales + row * (a.K / 128) + col / 128, lane);
+        }
+    }
+}
+
+struct WeightArgs {
+    const __bf16* w;
+    int64_t N, K;
+    int blocks_n, blocks_k;
+    uint8_t* codes;
+    float* scales;
+};
+
+// A 128 x 128 block to a workgroup: eight rows of 16-byte loads in each thread.
+__global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
+{
+    __shared__ uint32_t part[4];
+    const int64_t block = blockIdx.x;
+    const int64_t bk = block % a.blocks_k, en = block / a.blocks_k, expert = en / a.blocks_n, bn = en % a.blocks_n;
+    const int64_t row0 = bn * 128 + threadIdx.x / 16, at = (expert * a.N + row0) * a.K + bk * 128 + (threadIdx.x % 16) * 8;
+    float v[8][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        if (row0 + 16 * r < a.N) {
+            load8(a.w + at + 16 * r * a.K, v[r]);
+            m = max(m, amax8(v[r]));
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(part[0], part[1]), max(part[2], part[3]));
+    const float amax = __uint_as_float(max(m, kAmaxLeast)), inv = kE4m3Max / amax;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (row0 + 16 * r < a.N) *reinterpret_cast<v2i*>(a.codes + at + 16 * r * a.K) = codes8(v[r], inv);
+    if (threadIdx.x == 0) a.scales[block] = amax / kE4m3Max;
+}
+
+template <int T, int CH>
+hipError_t launch_norm(const NormArgs& a, hipStream_t st)
+{
+    hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fp8_quantize(const void* x, int64_t x_stride, int64_t rows, int64_t K, bool silu, void* codes, float* scales, hipStream_t st)
+{
+    const QuantArgs a{static_cast<const __bf16*>(x), x_stride, rows, K, static_cast<uint8_t*>(codes), scales};
+    const int64_t blocks = (rows * K / 8 + 255) / 256, most = (int64_t)compute_units() * 64;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (silu) hipLaunchKernelGGL(fp8_quantize_kernel<true>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(fp8_quantize_kernel<false>, grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t rows, int64_t K, float eps,
+                                       void* codes, float* scales, void* residual_out, void* norm_out, hipStream_t st)
+{
+    const NormArgs a{static_cast<const __bf16*>(x), static_cast<const __bf16*>(residual), static_cast<const __bf16*>(weight), static_cast<__bf16*>(residual_out),
+                     static_cast<__bf16*>(norm_out), static_cast<uint8_t*>(codes), scales, x_stride, rows, (int)K, eps};
+    const int64_t n8 = K / 8;
+    if (n8 <= 64) return launch_norm<64, 1>(a, st);
+    if (n8 <= 256) return launch_norm<256, 1>(a, st);
+    if (n8 <= 1024) return launch_norm<256, 4>(a, st);
+    if (n8 <= 2048) return launch_norm<1024, 2>(a, st);
+    return launch_norm<1024, 8>(a, st);
+}
+
+hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes, float* scales, hipStream_t st)
+{
+    WeightArgs a{static_cast<const __bf16*>(w), N, K, (int)((N + 127) / 128), (int)(K / 128), static_cast<uint8_t*>(codes), scales};
+    hipLaunchKernelGGL(fp8_quantize_weights_kernel, dim3((unsigned)(experts * a.blocks_n * a.blocks_k)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace fp4mr

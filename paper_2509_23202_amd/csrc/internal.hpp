@@ -164,6 +164,18 @@ hipError_t launch_gptq_hessian(const void* x, int64_t T, int64_t K, int b, float
 hipError_t launch_dequantize(const void* codes, const void* scales, const float* tensor_scale, int64_t rows, int64_t K, int mode,
                              bool gemm_layout, void* out, bool out_f32, hipStream_t st);
 
+// 8-bit operands (E4M3 codes, fp32 scales per 128): shapes and alignment as the C-ABI layer has checked them, K % 128 == 0
+hipError_t launch_fp8_quantize(const void* x, int64_t x_stride, int64_t rows, int64_t K, bool silu, void* codes, float* scales, hipStream_t st);
+// K <= kFp8NormMaxK; residual null or not, norm_out null or not
+constexpr int64_t kFp8NormMaxK = 65536;
+hipError_t launch_fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t rows, int64_t K, float eps,
+                                       void* codes, float* scales, void* residual_out, void* norm_out, hipStream_t st);
+hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes, float* scales, hipStream_t st);
+hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
+                           hipStream_t st);
+hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
+                                   const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
+
 hipError_t launch_probe(int which, void* buf, size_t bytes, int iters, hipStream_t st);
 
 }  // namespace fp4mr
