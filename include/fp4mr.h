@@ -367,7 +367,7 @@ fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* st
  *   scale = max(amax, 2^-100) / 448 ,  code = the E4M3 value nearest to  v * (448 / max(amax, 2^-100)) , ties to even ,
  * with amax the block's largest |v| and every operation in binary32.  A block that holds a NaN or an infinity has a scale that is
  * not finite, and every output of a product that reads it is NaN or infinite.
- * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24.  No rows (M, or rows, of 0) is not an
+ * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24, in products K <= 2^22 and M N <= 2^38.  No rows (M, or rows, of 0) is not an
  * error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.
  *
  * fp8_rmsnorm_quantize: codes, scales = Q(v),  v = h * weight / sqrt(mean(h^2) + eps),  h = bf16(x + residual), or x.

@@ -38,7 +38,9 @@ EXTRA_FLAGS = {"rotate_quantize.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                # (dequantized fragments come out of the vector ALU: as MFMA operands they should stay in vector registers)
                "gemm_nvfp4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "gemm_nv16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "gemm_nv_codes.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "gemm_nv_codes.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               # (the partial sums of a block are scaled in the vector ALU)
+               "fp8_gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> Path:

@@ -14,7 +14,11 @@ inline bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uint
 template <typename... P>
 bool aligned16(const P*... p) { return (aligned(p, 16) && ...); }
 
+// (products: K up to 2^22, so that 256 rows are within 2^30 bytes; an output of 2^38 elements is more than the memory of any device)
+constexpr int64_t kMostK = 1 << 22, kMostOutput = 1ll << 38;
+
 bool shape(int64_t M, int64_t N, int64_t K) { return M >= 0 && M <= kMost && N > 0 && N <= kMost && K > 0 && K <= kMost && K % 128 == 0; }
+bool product(int64_t M, int64_t N, int64_t K) { return shape(M, N, K) && K <= kMostK && M <= kMostOutput / N; }
 
 fp4mr_status_t status(hipError_t e) { return e == hipSuccess ? FP4MR_OK : FP4MR_ERR_DEVICE; }
 
@@ -58,7 +62,7 @@ fp4mr_status_t fp8_gemm(const void* a_codes, const float* a_scales, const void* 
                         uint32_t flags, void* stream)
 {
     if (flags & ~(uint32_t)FP4MR_OUT_F32) return FP4MR_ERR_FMT;
-    if (!shape(M, N, K)) return FP4MR_ERR_SHAPE;
+    if (!product(M, N, K)) return FP4MR_ERR_SHAPE;
     if (M == 0) return FP4MR_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return FP4MR_ERR_NULL;
     if (!aligned16(a_codes, a_scales, w_codes, w_scales, out)) return FP4MR_ERR_ALIGN;
@@ -69,7 +73,7 @@ fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int6
                                 const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, uint32_t flags, void* stream)
 {
     if (flags & ~(uint32_t)FP4MR_OUT_F32) return FP4MR_ERR_FMT;
-    if (!shape(rows, N, K) || !shape(a_rows, N, K) || experts <= 0 || experts > (1 << 16)) return FP4MR_ERR_SHAPE;
+    if (!product(rows, N, K) || !shape(a_rows, N, K) || experts <= 0 || experts > (1 << 16)) return FP4MR_ERR_SHAPE;
     if (index ? (rows > 0 && a_rows == 0) : a_rows != rows) return FP4MR_ERR_SHAPE;
     if (rows == 0) return FP4MR_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !offsets || !out) return FP4MR_ERR_NULL;

@@ -14,6 +14,7 @@
 #include "internal.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fp4mr {
 namespace {
@@ -69,116 +70,670 @@ struct Rows {
     int expert, begin, end;    // rows begin .. end - 1 of the output; none: begin == end
 };
 
-// The tile-th tile of R rows: tiles never span experts, and those of an expert follow one another.  What the offsets hold is kept within
-// the output, whatever it is.
-__device__ __forceinline__ Rows find_rows(const Fp8Args& g, int tile, int R)
+// Rows of expert base + lane, kept within the output whatever the offsets hold, and the inclusive sum over the lanes of their tiles of R rows.
+struct ExpertTiles {
+    int lo, hi, upto;
+};
+__device__ __forceinline__ ExpertTiles expert_tiles(const Fp8Args& g, int base, int R)
 {
-    const int lane = threadIdx.x & 63, T = (int)g.rows;
+    const int lane = threadIdx.x & 63, T = (int)g.rows, e = base + lane;
+    ExpertTiles x{0, 0, 0};
+    if (e < g.experts) {
+        x.lo = min(max(g.offsets[e], 0), T);
+        x.hi = min(max(g.offsets[e + 1], x.lo), T);
+    }
+    x.upto = (x.hi - x.lo + R - 1) / R;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int t = __shfl_up(x.upto, d);
+        if (lane >= d) x.upto += t;
+    }
+    return x;
+}
+
+// Tiles of R rows of all experts: tiles never span experts, and those of an expert follow one another.
+__device__ __forceinline__ int count_tiles(const Fp8Args& g, int R)
+{
+    int n = 0;
+    for (int base = 0; base < g.experts; base += 64) n += __shfl(expert_tiles(g, base, R).upto, 63);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+__device__ __forceinline__ Rows find_tile(const Fp8Args& g, int tile, int R)
+{
     int before = 0;
     for (int base = 0; base < g.experts; base += 64) {
-        const int e = base + lane;
-        int lo = 0, hi = 0;
-        if (e < g.experts) {
-            lo = min(max(g.offsets[e], 0), T);
-            hi = min(max(g.offsets[e + 1], lo), T);
-        }
-        const int tiles = (hi - lo + R - 1) / R;
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int t = __shfl_up(upto, d);
-            if (lane >= d) upto += t;
-        }
-        const uint64_t here = __ballot(tile < before + upto);
+        const ExpertTiles x = expert_tiles(g, base, R);
+        const uint64_t here = __ballot(tile < before + x.upto);
         if (here) {
-            const int l = __builtin_ctzll(here);
-            const int first = __shfl(lo, l) + (tile - before - __shfl(upto - tiles, l)) * R;
-            return Rows{base + l, first, min(first + R, __shfl(hi, l))};
+            const int l = __builtin_ctzll(here), earlier = l ? __shfl(x.upto, l - 1) : 0;
+            const int first = __shfl(x.lo, l) + (tile - before - earlier) * R;
+            return Rows{__builtin_amdgcn_readfirstlane(base + l), __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(min(first + R, __shfl(x.hi, l)))};
         }
-        before += __shfl(upto, 63);
+        before += __shfl(x.upto, 63);
     }
     return Rows{0, 0, 0};
 }
 
-// Sixteen columns and 16 TM rows to a workgroup, whose waves take the blocks of K in turn.
-template <bool GROUPED, bool OUT_F32, int TM, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void fp8_stream_kernel(Fp8Args g)
+constexpr uint32_t kOutside = 0xf0000000u;    // an offset past every operand, to which K may be added
+constexpr uint32_t kPast = 0x08000000u;       // past all activations' scales (4 / 128 of kOutside), and kOutside may be added
+
+// What the pieces of a row are exchanged by: the sixteen rows of a fragment, which lie next to each other (X) or four by four, sixteen apart (W), have every
+// pair of key and row % 2 once.
+__device__ __forceinline__ int x_key(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int w_key(int row) { return ((row >> 1) & 1) | (row / 16 & 3) << 1; }
+
+// A copy of a lane's number that the compiler takes for another one: what is computed from it stays where it is needed, once a tile, instead of in registers
+// throughout the main loop.
+__device__ __forceinline__ int kept_here(int lane)
 {
-    __shared__ v4f part[WAVES][TM][64];
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// 16 or 4 bytes of every lane to LDS, the lanes' one behind the other from `to`
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t from, char* smem, int to, uint32_t offset, int uniform_offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)((lds_char*)smem + to), 16, offset, uniform_offset, 0, 0);
+}
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, char* smem, int to, uint32_t offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)((lds_char*)smem + to), 4, offset, 0, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)(bytes > 0xffffffffll ? 0xffffffffu : (uint32_t)bytes), 0x00020000);
+}
+
+// ---------------------------------------------------------------- few rows: weights streamed from memory
+// 16 TN columns and 16 TM rows to a tile; a workgroup walks a run of tiles.  Its waves share K, each with a run of blocks; a block's codes and scales go to the
+// wave's own part of LDS by direct-to-LDS loads, D blocks ahead, the next tile's behind this one's, so that what is on its way never runs dry
+// and no wave waits for another but to add up a tile.
+template <int TM_, int TN_, int WAVES_, int D_>
+struct Stream {
+    static constexpr int TM = TM_, TN = TN_, WAVES = WAVES_, D = D_;
+    static constexpr int SLOT = (TN + TM) * 2048 + 256;      // W, A, and the scales: lane t 16 + r: of row r of A fragment t, lane 63: of W
+    static constexpr int LOADS = 2 * (TN + TM) + 1;
+    static constexpr int PART = WAVES * TM * TN * 1024;      // partial sums, of two tiles in turn
+    static constexpr int lds() { return WAVES * D * SLOT + 2 * PART; }
+    static_assert(TM <= 3 && lds() <= 163840 && D * LOADS < 64, "");
+};
+
+template <bool GROUPED, bool OUT_F32, typename C>
+__global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, int tiles_m, int tiles_n)
+{
+    constexpr int TM = C::TM, TN = C::TN, WAVES = C::WAVES, D = C::D;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int K = (int)g.K, KB = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
+    const bool gather = GROUPED && g.index != nullptr;
+    if constexpr (GROUPED) tiles_m = count_tiles(g, 16 * TM);
+    const int64_t ntiles = (int64_t)tiles_m * tiles_n;
+    const int tile_first = (int)(ntiles * blockIdx.x / gridDim.x), tile_end = (int)(ntiles * (blockIdx.x + 1) / gridDim.x);
+    if (tile_first >= tile_end) return;
+    const int each = (KB + WAVES - 1) / WAVES, kb_first = wave * each;
+
+    // ---- loads: block `kb` of tile `at`, and what goes with the tile.  Rows that it does not have lie outside of the operands: zeros.
+    const int ring = wave * D * C::SLOT;
+    const int piece = (lane & 7) ^ x_key(lane / 8);               // (rows r and r + 8 of sixteen: the key of the second is the first's + 4)
+    const uint32_t wo = (uint32_t)(lane / 8) * (uint32_t)K + piece * 16, wo8 = (uint32_t)(lane / 8 + 8) * (uint32_t)K + (piece ^ 4) * 16;
+    __amdgpu_buffer_rsrc_t rw, rx;
+    uint32_t xo[TM][2];
+    const float* scale = nullptr;
     Rows r{0, 0, 0};
-    if constexpr (GROUPED) {
-        r = find_rows(g, (int)blockIdx.y, 16 * TM);
-    } else {
-        r.begin = (int)blockIdx.y * 16 * TM;
-        r.end = min(r.begin + 16 * TM, (int)g.rows);
-    }
-    if (r.begin >= r.end) return;
-    const int KB = (int)(g.K >> 7), n0 = (int)blockIdx.x * 16, blocks_n = (int)((g.N + 127) >> 7);
-    const uint8_t* w = g.w + ((int64_t)r.expert * g.N + min((int64_t)n0 + (lane & 15), g.N - 1)) * g.K + (lane >> 4) * 16;
-    const float* ws = g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7)) * KB;
-    const uint8_t* a[TM];
-    const float* as[TM];
-    bool none[TM];
+    int n0 = 0, at_m = -1;
+    auto locate = [&](int tile) {
+        const int tm = tile / tiles_n;
+        n0 = (tile - tm * tiles_n) * 16 * TN;
+        if (tm != at_m) {
+            at_m = tm;
+            if constexpr (GROUPED) r = find_tile(g, tm, 16 * TM);
+            else r = Rows{0, tm * 16 * TM, min((tm + 1) * 16 * TM, (int)g.rows)};
+            const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;
+            rx = make_rsrc(g.a + x0 * K, x_rows * K);
+            auto x_row = [&](int m) -> int64_t {      // of A, from x0; outside: x_rows
+                const int64_t row = r.begin + m >= r.end ? -1 : gather ? g.index[r.begin + m] : m;
+                return row >= 0 && row < x_rows ? row : x_rows;
+            };
 #pragma unroll
-    for (int t = 0; t < TM; ++t) {
-        int64_t row = min(r.begin + 16 * t + (lane & 15), r.end - 1);
-        none[t] = false;
-        if (GROUPED && g.index) {
-            row = g.index[row];
-            none[t] = row < 0 || row >= g.a_rows;   // (a row of zeros)
-            if (none[t]) row = 0;
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t row = x_row(t * 16 + h * 8 + lane / 8);
+                    xo[t][h] = (row < x_rows ? (uint32_t)row * (uint32_t)K : kOutside) + (piece ^ (4 * h)) * 16;
+                }
+            int64_t row = x_row(min(lane, 16 * TM - 1));
+            if (row == x_rows) row = 0;               // (any: its codes are zeros, and the output's row is not stored or is set to zero)
+            scale = g.a_scales + (x0 + row) * KB;
         }
-        a[t] = g.a + row * g.K + (lane >> 4) * 16;
-        as[t] = g.a_scales + row * KB;
-    }
-    v4f acc[TM];
+        rw = make_rsrc(g.w + ((int64_t)r.expert * g.N + n0) * K, (int64_t)min((int)g.N - n0, 16 * TN) * K);
+        if (lane == 63) scale = g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7)) * KB;
+    };
+    int load_tile = tile_first, load_kb = 0, load_slot = 0;
+    auto issue = [&]() {
+        const int kb = min(kb_first + load_kb, KB - 1), to = ring + load_slot * C::SLOT;     // (past the last block: it again, with a scale of zero)
 #pragma unroll
-    for (int t = 0; t < TM; ++t) acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int kb = wave; kb < KB; kb += WAVES) {
-        const int64_t at = (int64_t)kb * 128;
-        const v4i wf[2] = {*reinterpret_cast<const v4i*>(w + at), *reinterpret_cast<const v4i*>(w + at + 64)};
-        const float sw = ws[kb];
+        for (int i = 0; i < TN; ++i) {
+            load_lds16(rw, smem, to + i * 2048, wo + (uint32_t)(16 * i) * (uint32_t)K, kb * 128);
+            load_lds16(rw, smem, to + i * 2048 + 1024, wo8 + (uint32_t)(16 * i) * (uint32_t)K, kb * 128);
+        }
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
-            const v4i af[2] = {*reinterpret_cast<const v4i*>(a[t] + at), *reinterpret_cast<const v4i*>(a[t] + at + 64)};
-            const float s = sw * as[t][kb];
-            const v4f p = OUT_F32 ? mfma_half(to_half(wf), to_half(af)) : mfma_fp8(wf, af);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(s, p[i], acc[t][i]);
+            load_lds16(rx, smem, to + (TN + t) * 2048, xo[t][0], kb * 128);
+            load_lds16(rx, smem, to + (TN + t) * 2048 + 1024, xo[t][1], kb * 128);
         }
-    }
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uintptr_t>(scale + kb)),
+                                         (lds_void*)((lds_char*)smem + to + (TN + TM) * 2048), 4, 0, 0);
+        load_slot = load_slot == D - 1 ? 0 : load_slot + 1;
+        if (++load_kb == each) {
+            load_kb = 0;
+            if (++load_tile < tile_end) locate(load_tile);      // (behind the last tile: its last block again, which nobody reads)
+            else load_kb = each - 1;
+        }
+    };
+    locate(tile_first);
 #pragma unroll
-    for (int t = 0; t < TM; ++t) part[wave][t][lane] = acc[t];
-    __syncthreads();
-    for (int t = wave; t < TM; t += WAVES) {
-        v4f sum = part[0][t][lane];
+    for (int d = 0; d < D - 1; ++d) issue();
+
+    // ---- products
+    const int l16 = lane & 15, f_at = l16 * 128 + ((lane >> 4) ^ x_key(l16)) * 16;
+    int slot = 0;
+    // what the tile that is multiplied has; the loads may be a tile or more ahead
+    Rows mine{0, 0, 0};
+    int mine_m = -1;
+    for (int tile = tile_first; tile < tile_end; ++tile) {
+        v4f acc[TM][TN];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += part[v][t][lane];
-        const int m = r.begin + 16 * t + (lane & 15);
-        if (m >= r.end) continue;
-        const bool zero = GROUPED && g.index && ((uint32_t)g.index[m] >= (uint64_t)g.a_rows);
-        const int64_t n = n0 + (lane >> 4) * 4, o = (int64_t)m * g.N + n;
+        for (int t = 0; t < TM; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (n + i < g.N) {
-                const float y = zero ? 0.0f : sum[i];
-                if constexpr (OUT_F32) static_cast<float*>(g.out)[o + i] = y;
-                else static_cast<__bf16*>(g.out)[o + i] = (__bf16)y;
+            for (int i = 0; i < TN; ++i) acc[t][i] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int k = 0; k < each; ++k) {
+            issue();
+            wait_vmcnt<(D - 1) * C::LOADS>();
+            asm volatile("" ::: "memory");
+            const char* from = smem + ring + slot * C::SLOT;
+            v4i wf[TN][2], af[TM][2];
+            float sa[TM];
+            auto read = [&](const char* p, v4i (&f)[2]) {
+                f[0] = *reinterpret_cast<const v4i*>(p + f_at);
+                f[1] = *reinterpret_cast<const v4i*>(p + (f_at ^ 64));
+            };
+#pragma unroll
+            for (int i = 0; i < TN; ++i) read(from + i * 2048, wf[i]);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                read(from + (TN + t) * 2048, af[t]);
+                sa[t] = reinterpret_cast<const float*>(from + (TN + TM) * 2048)[t * 16 + l16];
+            }
+            float sw = reinterpret_cast<const float*>(from + (TN + TM) * 2048)[63];
+            sw = kb_first + k < KB ? sw : 0.0f;
+            wait_lgkmcnt0();      // (the slot is loaded again by the next issue but D - 2)
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                const float s = kb_first + k < KB ? sw * sa[t] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < TN; ++i) {
+                    const v4f p = OUT_F32 ? mfma_half(to_half(wf[i]), to_half(af[t])) : mfma_fp8(wf[i], af[t]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][i][e] = fmaf(s, p[e], acc[t][i][e]);
+                }
+            }
+            slot = slot == D - 1 ? 0 : slot + 1;
+        }
+        // ---- the waves' sums in their order, and out
+        v4f* const part = reinterpret_cast<v4f*>(smem + WAVES * D * C::SLOT + ((tile - tile_first) & 1) * C::PART);
+#pragma unroll
+        for (int t = 0; t < TM; ++t)
+#pragma unroll
+            for (int i = 0; i < TN; ++i) part[(wave * TM * TN + t * TN + i) * 64 + lane] = acc[t][i];
+        wait_lgkmcnt0();
+        block_barrier();
+        const int tm = tile / tiles_n, col0 = (tile - tm * tiles_n) * 16 * TN;
+        if (tm != mine_m) {
+            mine_m = tm;
+            if constexpr (GROUPED) mine = find_tile(g, tm, 16 * TM);
+            else mine = Rows{0, tm * 16 * TM, min((tm + 1) * 16 * TM, (int)g.rows)};
+        }
+        for (int q = wave; q < TM * TN; q += WAVES) {
+            v4f sum = part[q * 64 + lane];
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) sum += part[(v * TM * TN + q) * 64 + lane];
+            const int m = mine.begin + 16 * (q / TN) + l16, n = col0 + 16 * (q % TN) + (lane >> 4) * 4;
+            if (m >= mine.end) continue;
+            if (gather && (uint32_t)g.index[m] >= (uint64_t)g.a_rows) sum = v4f{0.f, 0.f, 0.f, 0.f};
+            const int64_t o = (int64_t)m * g.N + n;
+            const int have = (int)g.N - n;
+            if constexpr (OUT_F32) {
+                float* const to = static_cast<float*>(g.out) + o;
+                if (have >= 4) __builtin_memcpy(to, &sum, 16);
+                else for (int e = 0; e < have; ++e) to[e] = sum[e];
+            } else {
+                const __bf16 y[4] = {(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]};
+                __bf16* const to = static_cast<__bf16*>(g.out) + o;
+                if (have >= 4) __builtin_memcpy(to, y, 8);      // (rows of an odd number of columns begin at any even byte)
+                else
+                    for (int e = 0; e < have; ++e) to[e] = e == 0 ? y[0] : e == 1 ? y[1] : y[2];
             }
         }
     }
+    wait_vmcnt<0>();    // (loads to LDS past the last block)
 }
 
-template <bool GROUPED>
-hipError_t launch(const Fp8Args& g, bool out_f32, hipStream_t st)
+// ---------------------------------------------------------------- tiles
+// BM x BN to a workgroup of NWM x NWN waves, each 16 TM x 64; a workgroup walks tiles.  A stage is 128 columns of both operands' rows in LDS, eight
+// rows to a 1 KB direct-to-LDS load; the sixteen-byte pieces of a row lie exchanged by a key, so that sixteen rows' reads of one piece touch
+// every bank once.  A step multiplies a stage: the W fragments stay in registers, the X fragments pass through two buffers, and the
+// products of one X fragment are added to the accumulators while the next one's run.  Before its last X fragment a wave has read all it needs
+// of the stage: there it waits for its loads of the next stage, the workgroup meets, and the last fragment's products cover the reads of the next
+// step's first fragments and the requests for the stage S steps on -- of the next tile, when this one's have all gone out: its first stages
+// are there before this tile's output has left.
+// The activations' scales take the same way four blocks of K at a time (a chunk; sixteen rows and four blocks to a load), in a ring of chunks: the
+// part of chunk c + 1 that goes out with the codes of step t = 4c .. 4c + 3 has landed by step t.  Parts past the last chunk go to a place that nobody
+// reads (every wave has the same number of loads on their way at any step: what the waits count).  With three slots they overwrite chunk c - 2, last read
+// in front of step 4c - 5, behind the meeting of step t - S >= 4c - 2 for S = 2; a new tile's first chunk goes out whole in front of its first codes, behind the
+// meeting of step K / 128 - S - 1, and the slots run on: for S = 2 its second chunk's parts begin behind that of step K / 128 - 2, when the last chunk but one of
+// the tile before has been read.  More stages have a fourth slot.
+template <int TM_, int NWM_, int NWN_, int STAGES_, int PER_CU_ = 1>
+struct Tile {
+    static constexpr int TM = TM_, TN = 4, NWM = NWM_, NWN = NWN_, S = STAGES_, NW = NWM * NWN, PER_CU = PER_CU_;
+    static constexpr int BM = 16 * TM * NWM, BN = 64 * NWN;
+    static constexpr int STAGE = (BM + BN) * 128, CHUNK = BM * 16, SLOTS = S == 2 ? 3 : 4;
+    static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL + 1;   // loads of a wave for a step: X, W, scales
+    static constexpr int NB = (BN + 127) / 128;
+    static constexpr int padded(int blocks) { return (blocks + 3) & ~3; }               // steps of a tile
+    static constexpr int out(bool f32) { return NW * 16 * 64 * (f32 ? 4 : 2); }
+    static constexpr int w_room(int blocks) { return (NB * blocks + 63) / 64 * 256; }   // the scales of W of a tile
+    static constexpr int lds(int blocks, bool f32) { return S * STAGE + SLOTS * CHUNK + 256 + out(f32) + 2 * w_room(blocks); }
+    // blocks of K that the scales of W have room for
+    static constexpr int max_blocks(bool f32) { return (163840 / PER_CU - lds(0, f32)) / 512 * 64 / NB; }
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 2 == 0 && BM <= 64 * NW && BM >= 64, "");
+    static constexpr bool ROLLED = TM >= 8;    // (see the kernel)
+    static_assert(S == (ROLLED ? 2 : 4) && (S - 1) * LPS < 64, "");
+};
+
+// Workgroups are dealt round-robin to the eight XCDs: each gets one contiguous range of tiles, in bands of four rows of tiles, so that those that share an
+// L2 share operands.
+__device__ __forceinline__ void place(int bid, int n, int tiles_m, int tiles_n, int& tm, int& tn)
 {
-    constexpr int TM = 4, WAVES = 8;
-    const int64_t tiles = GROUPED ? g.rows / (16 * TM) + std::min<int64_t>(g.experts, g.rows) : (g.rows + 16 * TM - 1) / (16 * TM);
-    const dim3 grid((unsigned)((g.N + 15) / 16), (unsigned)tiles);
-    if (out_f32) hipLaunchKernelGGL((fp8_stream_kernel<GROUPED, true, TM, WAVES>), grid, dim3(WAVES * 64), 0, st, g);
-    else hipLaunchKernelGGL((fp8_stream_kernel<GROUPED, false, TM, WAVES>), grid, dim3(WAVES * 64), 0, st, g);
+    const int per = n >> 3, rem = n & 7, xcd = bid & 7, idx = bid >> 3;
+    const int at = xcd < rem ? xcd * (per + 1) + idx : rem * (per + 1) + (xcd - rem) * per + idx;
+    const int band = 4 * tiles_n, first = at / band * 4, high = min(tiles_m - first, 4), in = at % band;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+template <bool GROUPED, bool OUT_F32, typename C>
+__global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void fp8_tile_kernel(Fp8Args g, int tiles_m, int tiles_n)
+{
+    constexpr int TM = C::TM, TN = C::TN, NW = C::NW, S = C::S, LPS = C::LPS;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    // places in LDS: the stages, then these
+    constexpr int kChunks = S * C::STAGE, kNowhere = kChunks + C::SLOTS * C::CHUNK, kRoom = kNowhere + 256, kWScales = kRoom + C::out(OUT_F32);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wm = wave % C::NWM, wn = wave / C::NWM;
+    const int K = (int)g.K, KB = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
+
+    if constexpr (GROUPED) tiles_m = count_tiles(g, C::BM);
+    const int ntiles = tiles_m * tiles_n;
+    int tile = blockIdx.x;
+    if (tile >= ntiles) return;
+
+    // ---- the tile whose operands are requested.  Rows that it does not have lie outside of the operand: their loads bring zeros, scales too.
+    const bool gather = GROUPED && g.index != nullptr;
+    Rows r{0, 0, 0};
+    int n0 = 0, w_side = 1;
+    __amdgpu_buffer_rsrc_t rx, rw, rs;
+    uint32_t xo[C::XL], wo[C::WL], so[4];
+    // ---- loads.  t: the step whose loads go out; its scales are a part of chunk t / 4 + 1, to slot t_slot, or where that is past the last one, nowhere.
+    // (Past the last step of the last tile its codes again, into a stage that nobody reads.)
+    int t = 0, t_slot = 0;
+    uint32_t t_block = 0;      // of a lane, among the chunk's four, as an offset
+    auto scale_block = [&](int chunk) { return 4 * chunk + (lane & 3) < KB ? (uint32_t)(4 * chunk + (lane & 3)) * 4 : kPast; };
+    constexpr bool ROLLED = C::ROLLED;
+    auto issue_scales = [&](int q, int to) {    // a part: by several waves, where there are fewer loads than waves, to the same end
+        load_lds4(rs, smem, to, so[q] + t_block);
+    };
+    const int part_at = wave % (C::BM / 64) * 256;
+    auto issue_step = [&](int stage, int q, int i) {
+        const int at = min(t, KB - 1) * 128;
+        if (i < C::XL) load_lds16(rx, smem, stage + (i * NW + wave) * 1024, xo[i < C::XL ? i : 0], at);
+        else if (i < LPS - 1) load_lds16(rw, smem, stage + C::BM * 128 + ((i - C::XL) * NW + wave) * 1024, wo[i < LPS - 1 && i >= C::XL ? i - C::XL : 0], at);
+        else issue_scales(ROLLED ? 0 : q, 4 * (t >> 2) + 4 < KB ? kChunks + t_slot * C::CHUNK + q * (C::BM / 64) * 256 + part_at : kNowhere);
+    };
+    auto next_slot = [](int slot) { return slot == C::SLOTS - 1 ? 0 : slot + 1; };
+    // In front of a tile's first codes: where its operands are, the scales of W, the first chunk.
+    auto begin_tile = [&]() {
+        const int lane = kept_here((int)threadIdx.x & 63);
+        int tm, tn;
+        place(tile, ntiles, tiles_m, tiles_n, tm, tn);
+        if constexpr (GROUPED) r = find_tile(g, tm, C::BM);
+        else r = Rows{0, tm * C::BM, min((tm + 1) * C::BM, (int)g.rows)};
+        n0 = tn * C::BN;
+        const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;
+        const int w_rows = min((int)g.N - n0, C::BN);
+        rx = make_rsrc(g.a + x0 * K, x_rows * K);
+        rs = make_rsrc(g.a_scales + x0 * KB, x_rows * KB * 4);
+        rw = make_rsrc(g.w + ((int64_t)r.expert * g.N + n0) * K, (int64_t)w_rows * K);
+        auto x_offset = [&](int m, int pitch) -> uint32_t {
+            const int row = r.begin + m >= r.end ? -1 : gather ? g.index[r.begin + m] : m;
+            return row >= 0 && row < x_rows ? (uint32_t)row * (uint32_t)pitch : kOutside;
+        };
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i) {
+            const int m = (i * NW + wave) * 8 + lane / 8;
+            xo[i] = x_offset(m, K) + (uint32_t)((lane & 7) ^ x_key(m)) * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < C::WL; ++i) {
+            const int n = (i * NW + wave) * 8 + lane / 8;
+            wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane & 7) ^ w_key(n)) * 16;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) so[q] = x_offset((q * (C::BM / 64) + wave % (C::BM / 64)) * 16 + lane / 4, KB * 4);
+
+        w_side ^= 1;
+        const int have = min(C::NB, blocks_n - (n0 >> 7)) * KB;
+        const __amdgpu_buffer_rsrc_t rsw = make_rsrc(g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7)) * KB, (int64_t)have * 4);
+        for (int i = wave * 64; i < have; i += NW * 64) load_lds4(rsw, smem, kWScales + w_side * C::w_room(KB) + i * 4, i + lane < have ? (uint32_t)(i + lane) * 4 : kOutside);
+        t = 0;
+        t_block = scale_block(0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) issue_scales(q, kChunks + t_slot * C::CHUNK + q * (C::BM / 64) * 256 + part_at);
+        t_slot = next_slot(t_slot);
+        t_block = scale_block(1);
+    };
+    // Behind the loads of a step.  fourth: t is now a multiple of four.
+    auto next_t = [&](bool fourth) {
+        ++t;
+        if constexpr (ROLLED) {
+            const uint32_t first = so[0];      // (part t % 4 of a chunk stays in front)
+            so[0] = so[1];
+            so[1] = so[2];
+            so[2] = so[3];
+            so[3] = first;
+        }
+        const bool on = fourth & (t < C::padded(KB));
+        t_slot = on ? next_slot(t_slot) : t_slot;
+        t_block = on ? scale_block((t >> 2) + 1) : t_block;
+    };
+
+    // ---- fragments: row l % 16 of X; for the i-th of W, of the wave's 64 columns that which leaves a lane sixteen consecutive ones of the output
+    const int l16 = lane & 15, xr = wm * TM * 16 + l16, wr = wn * 64 + l16 / 4 * 16 + l16 % 4;
+    const int xf_at = xr * 128 + ((lane >> 4) ^ x_key(xr)) * 16;
+    const int wf_at = C::BM * 128 + wr * 128 + ((lane >> 4) ^ w_key(wr)) * 16;    // (rows 4 i on have the same key)
+    auto read = [&](int at, int more, v4i (&f)[2]) {
+        f[0] = *reinterpret_cast<const v4i*>(smem + at + more);
+        f[1] = *reinterpret_cast<const v4i*>(smem + (at ^ 64) + more);
+    };
+    const int sx_at = kChunks + (wm * TM * 64 + l16 * 4) * 4;
+
+    begin_tile();
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st) {
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) issue_step(st * C::STAGE, st, i);
+        next_t(st == 3);
+    }
+    wait_vmcnt<(S - 2) * LPS>();
+    block_barrier();
+
+    // EARLY: a step begins with the meeting that frees the stage before it and says that the next one is there, and its last fragments' products cover the reads
+    // of the next step's first ones.  With two stages the meeting is in front of the last X fragment's products.
+    constexpr bool EARLY = S > 2;
+    constexpr int GROUPS = TM < 4 ? TM - 1 : 3, PER = (LPS + GROUPS - 1) / GROUPS, EACH_MFMA = (PER + TN - 1) / TN;   // a step's loads go out with so many X fragments
+    constexpr int RING = TM < 4 ? TM : 4, AHEAD = RING / 2;                          // X fragments are read so many of them ahead
+    v4i xf[RING][2], wf[TN][2];
+    constexpr bool SX4 = TM <= 4;          // a lane's scales of four steps in registers, for every X fragment
+    v4f sx4[SX4 ? TM : 1];
+    float sx[RING];                        // or those of the fragments that were read
+    int slot = 0, sw_at = kWScales + wn / 2 * KB * 4;
+    float sw = *reinterpret_cast<const float*>(smem + sw_at);
+#pragma unroll
+    for (int i = 0; i < TN; ++i) read(wf_at, i * 512, wf[i]);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+        read(xf_at, j * 2048, xf[j]);
+        if constexpr (!SX4) sx[j] = *reinterpret_cast<const float*>(smem + sx_at + j * 256);
+    }
+    if constexpr (SX4) {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) sx4[j] = *reinterpret_cast<const v4f*>(smem + sx_at + j * 256);
+    }
+
+    for (;;) {
+        const Rows here = r;       // (the loads move on to the next tile before this one is done)
+        const int here_n0 = n0, here_tile = tile;
+        // p: the products of the X fragment before (and of the present one, where there are the registers)
+        constexpr int P = TM >= 8 ? 1 : 2;
+        v4f acc[TM][TN], p[P][TN];
+        float s = 0.0f;            // their scale
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int i = 0; i < TN; ++i) acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < TN; ++i) p[P - 1][i] = v4f{0.f, 0.f, 0.f, 0.f};
+
+        // Step u of a chunk, 0 .. 3 (those past the last block add nothing: their scales are zeros): a constant where four steps are unrolled, so that a stage's
+        // places are too, or not, where that takes more registers than there are.
+        int steps = C::padded(KB), kt = 0;
+        asm volatile("" : "+s"(steps));    // (nothing that the compiler knows: every unrolled step is a block of its own to it, whose order it keeps)
+        auto step = [&](auto u) {
+            const int STAGE = u % S * C::STAGE, NEXT = (u + 1) % S * C::STAGE, FILL = (u + S - 1) % S * C::STAGE;
+            const int Q = (u + S - 1) % 4;         // the part of a chunk that goes out
+            const bool last = kt + 4 - u >= KB;    // this is the tile's last chunk
+            const int slot_next = next_slot(slot);
+            const int sw_next_at = u < 3 ? sw_at + 4 * (u + 1) : last ? kWScales + w_side * C::w_room(KB) + wn / 2 * KB * 4 : sw_at + 16;   // (the next tile's, when the loads are there)
+            auto meet = [&]() {
+                wait_vmcnt<(EARLY ? S - 3 : S - 2) * LPS>();
+                if constexpr (!EARLY) wait_lgkmcnt0();    // (early: what was read of the stage before has been multiplied)
+                block_barrier();
+            };
+            if constexpr (EARLY) meet();
+            Half32 wh[OUT_F32 ? TN : 1];
+            if constexpr (OUT_F32) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) wh[i] = to_half(wf[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                auto fetch = [&](int q) {     // X fragment q from the front of this stage
+                    read(xf_at, q < TM ? STAGE + q * 2048 : NEXT + (q - TM) * 2048, xf[q % RING]);
+                    if constexpr (!SX4) {
+                        const int at = q < TM ? slot * C::CHUNK + u * 4 : u < 3 ? slot * C::CHUNK + (u + 1) * 4 : slot_next * C::CHUNK;
+                        sx[q % RING] = *reinterpret_cast<const float*>(smem + sx_at + at + q % TM * 256);
+                    }
+                };
+                if (EARLY || j + AHEAD < TM) fetch(j + AHEAD);
+                float sw_next = sw;
+                if (j == TM - 1) {
+                    next_t(Q == 3);
+                    if constexpr (!EARLY) {
+                        meet();
+#pragma unroll
+                        for (int q = 0; q < AHEAD; ++q) fetch(TM + q);
+                    }
+                    sw_next = *reinterpret_cast<const float*>(smem + sw_next_at);
+                }
+                Half32 xh;
+                if constexpr (OUT_F32) xh = to_half(xf[j % RING]);
+#pragma unroll
+                for (int i = 0; i < TN; ++i) {
+                    v4f& to = acc[j == 0 ? TM - 1 : j - 1][i];
+                    auto add = [&](const v4f& q) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[e] = fmaf(s, q[e], to[e]);
+                    };
+                    if constexpr (P == 1) add(p[0][i]);
+                    if constexpr (OUT_F32) p[P == 1 ? 0 : j & 1][i] = mfma_half(wh[i], xh);
+                    else p[P == 1 ? 0 : j & 1][i] = mfma_fp8(wf[i], xf[j % RING]);
+                    if constexpr (P == 2) add(p[1 - (j & 1)][i]);
+                    if (j == TM - 1) read(wf_at, NEXT + i * 512, wf[i]);
+                    // (the order is kept: the additions of four products beside every MFMA, and a load or two)
+#pragma unroll
+                    for (int l = 0; l < EACH_MFMA; ++l)
+                        if (j < GROUPS && i * EACH_MFMA + l < PER && j * PER + i * EACH_MFMA + l < LPS) issue_step(FILL, Q, j * PER + i * EACH_MFMA + l);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (SX4) {
+                    s = sx4[j][(int)u] * sw;
+                    if (u == 3) sx4[j] = *reinterpret_cast<const v4f*>(smem + sx_at + slot_next * C::CHUNK + j * 256);
+                } else {
+                    s = sx[j % RING] * sw;
+                }
+                if (u > 0) s = kt < KB ? s : 0.0f;
+                sw = sw_next;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            ++kt;
+            if (u == 3) {
+                slot = slot_next;
+                sw_at = sw_next_at;
+            }
+        };
+        auto move_on = [&]() {     // the loads of this tile have gone out
+            if (tile + (int)gridDim.x < ntiles) {
+                tile += gridDim.x;
+                begin_tile();
+            }
+        };
+        if constexpr (ROLLED) {
+#pragma clang loop unroll(disable)
+            for (int part = 0; part < 2; ++part) {
+                int to = part ? steps : steps - S + 1;
+                asm volatile("" : "+s"(to));
+#pragma clang loop unroll(disable)
+                while (kt < to) step(kt & 3);
+                if (part == 0) move_on();
+            }
+        } else {
+            while (kt < steps) {
+                const bool last = kt + 4 >= steps;
+                step(std::integral_constant<int, 0>{});
+#pragma unroll
+                for (int j = 0; j < TM; ++j)     // (the step's products are not to be computed behind the branch)
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) asm volatile("" : "+v"(acc[j][i]));
+#pragma unroll
+                for (int i = 0; i < TN; ++i) asm volatile("" : "+v"(p[P - 1][i]));
+                if (last) move_on();
+                if (kt < steps) step(std::integral_constant<int, 1>{});
+                if (kt < steps) step(std::integral_constant<int, 2>{});
+                if (kt < steps) step(std::integral_constant<int, 3>{});
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[TM - 1][i][e] = fmaf(s, p[P - 1][i][e], acc[TM - 1][i][e]);
+
+        // ---- output: sixteen rows at a time through 16 x 64 elements of LDS of the wave's own, so that a row leaves as whole lines
+        typedef std::conditional_t<OUT_F32, float, __bf16> Out;
+        const int lane = kept_here((int)threadIdx.x & 63), l16 = lane & 15;
+        constexpr int EACH = 16 / sizeof(Out), PIECES = 64 / EACH, ROWS = 64 / PIECES;     // pieces of a row; rows to a store
+        auto key = [](int row) { return OUT_F32 ? row & 15 : row >> 1 & 7; };
+        char* const room = smem + kRoom + wave * (C::out(OUT_F32) / NW);
+        const int row0 = here.begin + wm * TM * 16 + lane / PIECES, col = here_n0 + wn * 64 + lane % PIECES * EACH, have = (int)g.N - col;
+        const bool inside = here.begin + (wm + 1) * TM * 16 <= here.end && here_n0 + wn * 64 + 64 <= (int)g.N;
+        Out* out = static_cast<Out*>(g.out) + (int64_t)row0 * g.N + col;
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+#pragma unroll
+            for (int i = 0; i < TN; i += 8 / EACH == 2 ? 1 : 2) {
+                const int piece = (lane >> 4) * (16 / EACH) + i * 4 / EACH;
+                char* const to = room + l16 * (PIECES * 16) + (piece ^ key(l16)) * 16;
+                if constexpr (OUT_F32) {
+                    *reinterpret_cast<v4f*>(to) = acc[j][i];
+                } else {
+                    *reinterpret_cast<v8bf*>(to) = v8bf{(__bf16)acc[j][i][0], (__bf16)acc[j][i][1], (__bf16)acc[j][i][2], (__bf16)acc[j][i][3],
+                                                        (__bf16)acc[j][i + 1][0], (__bf16)acc[j][i + 1][1], (__bf16)acc[j][i + 1][2], (__bf16)acc[j][i + 1][3]};
+                }
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int h = 0; h < 16 / ROWS; ++h) {
+                const int row = h * ROWS + lane / PIECES;
+                const v4i y = *reinterpret_cast<const v4i*>(room + row * (PIECES * 16) + (lane % PIECES ^ key(row)) * 16);
+                // (rows of an odd number of columns begin at any even byte)
+                if (inside) {
+                    __builtin_memcpy(out, &y, 16);
+                } else if (row0 + 16 * j + h * ROWS < here.end) {
+                    if (have >= EACH) {
+                        __builtin_memcpy(out, &y, 16);
+                    } else {
+                        const Out* const from = reinterpret_cast<const Out*>(room + row * (PIECES * 16) + (lane % PIECES ^ key(row)) * 16);
+#pragma clang loop unroll(disable) vectorize(disable)
+                        for (int e = 0; e < have; ++e) out[e] = from[e];
+                    }
+                }
+                out += ROWS * g.N;
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (tile == here_tile) break;
+    }
+    wait_vmcnt<0>();    // (loads to LDS past the last step)
+}
+
+template <bool GROUPED, bool OUT_F32, typename C>
+hipError_t launch_tile(const Fp8Args& g, hipStream_t st)
+{
+    static LdsAttrOnce attr;
+    const int KB = (int)(g.K >> 7);
+    const hipError_t e = attr.ensure(reinterpret_cast<const void*>(fp8_tile_kernel<GROUPED, OUT_F32, C>), 163840 / C::PER_CU);
+    if (e != hipSuccess) return e;
+    const int64_t tiles_m = GROUPED ? g.rows / C::BM + std::min<int64_t>(g.experts, g.rows) : (g.rows + C::BM - 1) / C::BM, tiles_n = (g.N + C::BN - 1) / C::BN;
+    const int64_t grid = std::min<int64_t>(tiles_m * tiles_n, (int64_t)compute_units() * C::PER_CU);
+    hipLaunchKernelGGL((fp8_tile_kernel<GROUPED, OUT_F32, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(KB, OUT_F32), st, g, (int)tiles_m, (int)tiles_n);
     return hipGetLastError();
+}
+
+template <bool GROUPED, bool OUT_F32, typename C>
+hipError_t launch_stream(const Fp8Args& g, hipStream_t st)
+{
+    static LdsAttrOnce attr;
+    const hipError_t e = attr.ensure(reinterpret_cast<const void*>(fp8_stream_kernel<GROUPED, OUT_F32, C>), C::lds());
+    if (e != hipSuccess) return e;
+    const int64_t tiles_m = GROUPED ? g.rows / (16 * C::TM) + std::min<int64_t>(g.experts, g.rows) : (g.rows + 16 * C::TM - 1) / (16 * C::TM), tiles_n = (g.N + 16 * C::TN - 1) / (16 * C::TN);
+    const int64_t per_cu = 163840 / C::lds(), grid = std::min<int64_t>(tiles_m * tiles_n, compute_units() * per_cu);
+    hipLaunchKernelGGL((fp8_stream_kernel<GROUPED, OUT_F32, C>), dim3((unsigned)grid), dim3(C::WAVES * 64), C::lds(), st, g, (int)tiles_m, (int)tiles_n);
+    return hipGetLastError();
+}
+
+typedef Tile<8, 2, 4, 2> Tile256;           // 256 x 256
+typedef Tile<4, 2, 2, 4> Tile128;           // 128 x 128
+typedef Tile<2, 2, 2, 4> Tile64;            // 64 x 128
+typedef Tile<2, 4, 2, 4> TileX;            // 128 x 128, 8 waves
+
+template <bool GROUPED, bool OUT_F32, typename C>
+bool tile_takes(const Fp8Args& g)
+{
+    const int64_t KB = g.K >> 7;
+    return KB >= 4 && KB <= C::max_blocks(OUT_F32) && !(GROUPED && g.index && g.a_rows * g.K > (int64_t)kOutside);
+}
+
+template <bool GROUPED, bool OUT_F32>
+hipError_t launch(const Fp8Args& g, hipStream_t st)
+{
+    const int variant = options().gemm_variant;
+    if constexpr (!OUT_F32) if (variant == 1 && tile_takes<GROUPED, OUT_F32, Tile256>(g)) return launch_tile<GROUPED, OUT_F32, Tile256>(g, st);
+    if constexpr (!OUT_F32) if (variant == 2 && tile_takes<GROUPED, OUT_F32, Tile128>(g)) return launch_tile<GROUPED, OUT_F32, Tile128>(g, st);
+    if (variant == 4 && tile_takes<GROUPED, OUT_F32, TileX>(g)) return launch_tile<GROUPED, OUT_F32, TileX>(g, st);
+    if (variant == 3 && tile_takes<GROUPED, OUT_F32, Tile64>(g)) return launch_tile<GROUPED, OUT_F32, Tile64>(g, st);
+    if (variant == 10) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 8, 4>>(g, st);
+    if (variant == 11) return launch_stream<GROUPED, OUT_F32, Stream<1, 2, 4, 5>>(g, st);
+    if (variant == 12) return launch_stream<GROUPED, OUT_F32, Stream<2, 1, 4, 5>>(g, st);
+    if (variant == 13) return launch_stream<GROUPED, OUT_F32, Stream<2, 2, 4, 3>>(g, st);
+    if (variant == 14) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 4, 4>>(g, st);
+    if (variant == 15) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 4, 8>>(g, st);
+    if (variant == 16) return launch_stream<GROUPED, OUT_F32, Stream<2, 1, 8, 2>>(g, st);
+    if (variant == 17) return launch_stream<GROUPED, OUT_F32, Stream<1, 2, 8, 2>>(g, st);
+    return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 8, 4>>(g, st);
 }
 
 }  // namespace
@@ -186,14 +741,15 @@ hipError_t launch(const Fp8Args& g, bool out_f32, hipStream_t st)
 hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
                            hipStream_t st)
 {
-    return launch<false>(Fp8Args{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, M, N, K, M, nullptr, nullptr, 1}, out_f32, st);
+    const Fp8Args g{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, M, N, K, M, nullptr, nullptr, 1};
+    return out_f32 ? launch<false, true>(g, st) : launch<false, false>(g, st);
 }
 
 hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st)
 {
-    return launch<true>(Fp8Args{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, a_rows, N, K, rows, offsets, index, (int)experts},
-                        out_f32, st);
+    const Fp8Args g{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, a_rows, N, K, rows, offsets, index, (int)experts};
+    return out_f32 ? launch<true, true>(g, st) : launch<true, false>(g, st);
 }
 
 }  // namespace fp4mr
