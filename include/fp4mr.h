@@ -333,8 +333,10 @@ fp4mr_status_t fp4_dequantize(const void* codes, const void* scales, const float
  *   FP4MR_OPT_GEMM_GRID     0 (default): one persistent workgroup per compute unit; n > 0: at most n workgroups
  *   FP4MR_OPT_SW_CODEC      1: the quantizers encode E2M1 / E4M3 with integer arithmetic instead of the converting
  *                           instructions (same results bit for bit; abs-max and 4/3 policies only)
+ *   FP4MR_OPT_FP8_VARIANT   0 (default): fp8_gemm and fp8_grouped_gemm pick their kernel; 1..7: force one of few rows or of tiles, 8..13: fp8_gemm in
+ *                           2, 4 or 8 parts of K where the workspace holds their sums (products that a forced kernel does not take run on another)
  */
-enum { FP4MR_OPT_GEMM_VARIANT = 0, FP4MR_OPT_GEMM_GRID = 1, FP4MR_OPT_SW_CODEC = 2 };
+enum { FP4MR_OPT_GEMM_VARIANT = 0, FP4MR_OPT_GEMM_GRID = 1, FP4MR_OPT_SW_CODEC = 2, FP4MR_OPT_FP8_VARIANT = 3 };
 fp4mr_status_t fp4_set_option(int option, int value);
 
 /*
@@ -398,9 +400,13 @@ fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, i
  * scales.  out is bf16, or fp32 with FP4MR_OUT_F32.  For a bf16 output the 8-bit matrix instruction sums eight products at a time and drops what
  * lies below 2^-13 of the largest of them: an output is within (2^-10 + K 2^-31 + 2^-16) sum |a w| of the exact product before its rounding.  For an fp32
  * output the codes are multiplied as fp16 with fp32 sums, at less than half the rate: within (K / 128 + 129) 2^-24 sum |a w|.
+ *   workspace    optional: with fp8_workspace_bytes(M, N, K, flags) bytes (0 where that is of no use) a product of few tiles and a long K is split
+ *                along K over otherwise idle compute units, and its parts' fp32 sums, kept there, are added in a fixed order.  With less, or
+ *                NULL, it runs in fewer parts, or in one.  Results of different plans differ in the order of their sums.
  */
 fp4mr_status_t fp8_gemm(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales, int64_t M, int64_t N,
-                        int64_t K, void* out, uint32_t flags, void* stream);
+                        int64_t K, void* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+size_t fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, uint32_t flags);
 
 /*
  * The same with rows grouped by expert: rows offsets[e] .. offsets[e+1] - 1 of out are those rows of A times the weights of expert e.

@@ -35,7 +35,7 @@ FIT_RANGE_FLOATS = 258
 SILU_MUL = 1 << 12
 A_SCALE43 = 1 << 8
 W_SCALE43 = 1 << 9
-OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC = 0, 1, 2
+OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC, OPT_FP8_VARIANT = 0, 1, 2, 3
 OP_ROTATE_QUANTIZE, OP_QUANTIZE_WEIGHTS, OP_GEMM, OP_GPTQ, OP_GPTQ_PREPARE, OP_GPTQ_HESSIAN, OP_GEMM_SPLIT_K, OP_GEMM_FASTEST = 0, 1, 2, 3, 4, 5, 6, 7
 
 _p, _i64, _i32, _u32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_uint32, ctypes.c_size_t
@@ -77,7 +77,9 @@ lib.fp8_quantize.argtypes = [_p, _i64, _i64, _i64, _p, _p, _u32, _p]
 lib.fp8_quantize.restype = _i32
 lib.fp8_quantize_weights.argtypes = [_p, _i64, _i64, _i64, _p, _p, _u32, _p]
 lib.fp8_quantize_weights.restype = _i32
-lib.fp8_gemm.argtypes = [_p, _p, _p, _p, _i64, _i64, _i64, _p, _u32, _p]
+lib.fp8_gemm.argtypes = [_p, _p, _p, _p, _i64, _i64, _i64, _p, _p, _sz, _u32, _p]
+lib.fp8_workspace_bytes.argtypes = [_i64, _i64, _i64, _u32]
+lib.fp8_workspace_bytes.restype = _sz
 lib.fp8_gemm.restype = _i32
 lib.fp8_grouped_gemm.argtypes = [_p, _p, _i64, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _p, _u32, _p]
 lib.fp8_grouped_gemm.restype = _i32
@@ -429,12 +431,20 @@ def _product_out(a_codes, a_scales, w_codes, w_scales, dim: int, rows: int, flag
     return out, N, K
 
 
-def fp8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None):
+def fp8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None, workspace=None):
     """out[M,N] = A W^T (bf16, or fp32 with OUT_F32) from the codes and scales of activations [M,K] and weights [N,K]."""
     M = a_codes.shape[0]
     out, N, K = _product_out(a_codes, a_scales, w_codes, w_scales, 2, M, flags, out)
-    _check(lib.fp8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, out.data_ptr(), flags, _stream()))
+    need = fp8_workspace_bytes(M, N, K, flags)
+    if need and workspace is None:
+        workspace = (a_codes.new_empty if type(a_codes) is _Tensor else _plain_empty(a_codes))(need, dtype=torch.uint8)
+    wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.fp8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, out.data_ptr(), _ptr(workspace), wsz, flags, _stream()))
     return out
+
+
+def fp8_workspace_bytes(M: int, N: int, K: int, flags: int = 0) -> int:
+    return int(lib.fp8_workspace_bytes(M, N, K, flags))
 
 
 def fp8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=None, flags: int = 0, out=None):

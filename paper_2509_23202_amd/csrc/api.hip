@@ -157,6 +157,10 @@ fp4mr_status_t fp4_set_option(int option, int value)
         case FP4MR_OPT_SW_CODEC:
             o.sw_codec = value != 0;
             return FP4MR_OK;
+        case FP4MR_OPT_FP8_VARIANT:
+            if (value < 0 || value > kMaxFp8Variant) return FP4MR_ERR_FMT;
+            o.fp8_variant = value;
+            return FP4MR_OK;
         default: return FP4MR_ERR_FMT;
     }
 }

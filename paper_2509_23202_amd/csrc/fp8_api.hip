@@ -59,14 +59,20 @@ fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, i
 }
 
 fp4mr_status_t fp8_gemm(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out,
-                        uint32_t flags, void* stream)
+                        void* workspace, size_t workspace_bytes, uint32_t flags, void* stream)
 {
     if (flags & ~(uint32_t)FP4MR_OUT_F32) return FP4MR_ERR_FMT;
     if (!product(M, N, K)) return FP4MR_ERR_SHAPE;
     if (M == 0) return FP4MR_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return FP4MR_ERR_NULL;
-    if (!aligned16(a_codes, a_scales, w_codes, w_scales, out)) return FP4MR_ERR_ALIGN;
-    return status(launch_fp8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, out, (flags & FP4MR_OUT_F32) != 0, static_cast<hipStream_t>(stream)));
+    if (!aligned16(a_codes, a_scales, w_codes, w_scales, out, workspace)) return FP4MR_ERR_ALIGN;
+    return status(launch_fp8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, out, (flags & FP4MR_OUT_F32) != 0, workspace, workspace ? workspace_bytes : 0,
+                                  static_cast<hipStream_t>(stream)));
+}
+
+size_t fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, uint32_t flags)
+{
+    return M > 0 && product(M, N, K) ? fp8_gemm_partial_bytes(M, N, K, (flags & FP4MR_OUT_F32) != 0) : 0;
 }
 
 fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int64_t a_rows, const void* w_codes, const float* w_scales, const int32_t* offsets,

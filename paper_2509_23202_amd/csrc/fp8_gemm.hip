@@ -14,6 +14,7 @@
 #include "internal.hpp"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace fp4mr {
@@ -365,57 +366,72 @@ __device__ __forceinline__ void place(int bid, int n, int tiles_m, int tiles_n, 
     tn = in / high;
 }
 
-template <bool GROUPED, bool OUT_F32, typename C>
-__global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void fp8_tile_kernel(Fp8Args g, int tiles_m, int tiles_n)
+// EXACT: fp32 sums (the fp16 MFMA); OUT_F32: they leave as fp32.  SPLIT: a unit of work is one part of K of a tile, each of part_blocks blocks but the last, and
+// what leaves is its sums, to the part's own copy of the output.
+template <bool GROUPED, bool EXACT, bool OUT_F32, bool SPLIT, typename C>
+__global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void fp8_tile_kernel(Fp8Args g, int tiles_m, int tiles_n, int split_parts, int split_blocks)
 {
+    static_assert(!SPLIT || (OUT_F32 && !GROUPED), "");
+    const int parts = SPLIT ? split_parts : 1, part_blocks = SPLIT ? split_blocks : (int)(g.K >> 7);
     constexpr int TM = C::TM, TN = C::TN, NW = C::NW, S = C::S, LPS = C::LPS;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     // places in LDS: the stages, then these
     constexpr int kChunks = S * C::STAGE, kNowhere = kChunks + C::SLOTS * C::CHUNK, kRoom = kNowhere + 256, kWScales = kRoom + C::out(OUT_F32);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave % C::NWM, wn = wave / C::NWM;
-    const int K = (int)g.K, KB = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
+    const int K = (int)g.K, KS = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
 
     if constexpr (GROUPED) tiles_m = count_tiles(g, C::BM);
-    const int ntiles = tiles_m * tiles_n;
+    const int ntiles = tiles_m * tiles_n * parts;
     int tile = blockIdx.x;
     if (tile >= ntiles) return;
 
     // ---- the tile whose operands are requested.  Rows that it does not have lie outside of the operand: their loads bring zeros, scales too.
     const bool gather = GROUPED && g.index != nullptr;
     Rows r{0, 0, 0};
-    int n0 = 0, w_side = 1;
+    int n0 = 0, w_side = 1, part = 0, part_k0 = 0, part_n = 0;
+    auto k0 = [&]() { return SPLIT ? part_k0 : 0; };     // its blocks of K: KB() of them from k0() on
+    auto KB = [&]() { return SPLIT ? part_n : KS; };
     __amdgpu_buffer_rsrc_t rx, rw, rs;
     uint32_t xo[C::XL], wo[C::WL], so[4];
     // ---- loads.  t: the step whose loads go out; its scales are a part of chunk t / 4 + 1, to slot t_slot, or where that is past the last one, nowhere.
     // (Past the last step of the last tile its codes again, into a stage that nobody reads.)
     int t = 0, t_slot = 0;
     uint32_t t_block = 0;      // of a lane, among the chunk's four, as an offset
-    auto scale_block = [&](int chunk) { return 4 * chunk + (lane & 3) < KB ? (uint32_t)(4 * chunk + (lane & 3)) * 4 : kPast; };
+    auto scale_block = [&](int chunk) { return 4 * chunk + (lane & 3) < KB() ? (uint32_t)(k0() + 4 * chunk + (lane & 3)) * 4 : kPast; };
     constexpr bool ROLLED = C::ROLLED;
     auto issue_scales = [&](int q, int to) {    // a part: by several waves, where there are fewer loads than waves, to the same end
         load_lds4(rs, smem, to, so[q] + t_block);
     };
     const int part_at = wave % (C::BM / 64) * 256;
     auto issue_step = [&](int stage, int q, int i) {
-        const int at = min(t, KB - 1) * 128;
+        const int at = (k0() + min(t, KB() - 1)) * 128;
         if (i < C::XL) load_lds16(rx, smem, stage + (i * NW + wave) * 1024, xo[i < C::XL ? i : 0], at);
         else if (i < LPS - 1) load_lds16(rw, smem, stage + C::BM * 128 + ((i - C::XL) * NW + wave) * 1024, wo[i < LPS - 1 && i >= C::XL ? i - C::XL : 0], at);
-        else issue_scales(ROLLED ? 0 : q, 4 * (t >> 2) + 4 < KB ? kChunks + t_slot * C::CHUNK + q * (C::BM / 64) * 256 + part_at : kNowhere);
+        else issue_scales(ROLLED ? 0 : q, 4 * (t >> 2) + 4 < KB() ? kChunks + t_slot * C::CHUNK + q * (C::BM / 64) * 256 + part_at : kNowhere);
     };
     auto next_slot = [](int slot) { return slot == C::SLOTS - 1 ? 0 : slot + 1; };
     // In front of a tile's first codes: where its operands are, the scales of W, the first chunk.
     auto begin_tile = [&]() {
         const int lane = kept_here((int)threadIdx.x & 63);
         int tm, tn;
-        place(tile, ntiles, tiles_m, tiles_n, tm, tn);
+        if constexpr (!SPLIT) {
+            place(tile, ntiles, tiles_m, tiles_n, tm, tn);
+        } else {       // (neighbours of different parts, so that with eight parts an XCD has one part of K of both operands)
+            const int at = tile / parts;
+            part = tile - at * parts;
+            tn = at / tiles_m;
+            tm = at - tn * tiles_m;
+            part_k0 = part * part_blocks;
+            part_n = min(part_blocks, KS - part_k0);
+        }
         if constexpr (GROUPED) r = find_tile(g, tm, C::BM);
         else r = Rows{0, tm * C::BM, min((tm + 1) * C::BM, (int)g.rows)};
         n0 = tn * C::BN;
         const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;
         const int w_rows = min((int)g.N - n0, C::BN);
         rx = make_rsrc(g.a + x0 * K, x_rows * K);
-        rs = make_rsrc(g.a_scales + x0 * KB, x_rows * KB * 4);
+        rs = make_rsrc(g.a_scales + x0 * KS, x_rows * KS * 4);
         rw = make_rsrc(g.w + ((int64_t)r.expert * g.N + n0) * K, (int64_t)w_rows * K);
         auto x_offset = [&](int m, int pitch) -> uint32_t {
             const int row = r.begin + m >= r.end ? -1 : gather ? g.index[r.begin + m] : m;
@@ -432,12 +448,16 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
             wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane & 7) ^ w_key(n)) * 16;
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) so[q] = x_offset((q * (C::BM / 64) + wave % (C::BM / 64)) * 16 + lane / 4, KB * 4);
+        for (int q = 0; q < 4; ++q) so[q] = x_offset((q * (C::BM / 64) + wave % (C::BM / 64)) * 16 + lane / 4, KS * 4);
 
         w_side ^= 1;
-        const int have = min(C::NB, blocks_n - (n0 >> 7)) * KB;
-        const __amdgpu_buffer_rsrc_t rsw = make_rsrc(g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7)) * KB, (int64_t)have * 4);
-        for (int i = wave * 64; i < have; i += NW * 64) load_lds4(rsw, smem, kWScales + w_side * C::w_room(KB) + i * 4, i + lane < have ? (uint32_t)(i + lane) * 4 : kOutside);
+        // (of one part of K: a row of the scales at a time, else all rows, which lie behind one another)
+        const int have = SPLIT ? KB() : min(C::NB, blocks_n - (n0 >> 7)) * KB();
+        for (int nb = 0; nb < (SPLIT ? min(C::NB, blocks_n - (n0 >> 7)) : 1); ++nb) {
+            const __amdgpu_buffer_rsrc_t rsw = make_rsrc(g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7) + nb) * KS + k0(), (int64_t)have * 4);
+            for (int i = wave * 64; i < have; i += NW * 64)
+                if (i + lane < have) load_lds4(rsw, smem, kWScales + w_side * C::w_room(part_blocks) + (nb * part_blocks + i) * 4, (uint32_t)(i + lane) * 4);
+        }
         t = 0;
         t_block = scale_block(0);
 #pragma unroll
@@ -455,7 +475,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
             so[2] = so[3];
             so[3] = first;
         }
-        const bool on = fourth & (t < C::padded(KB));
+        const bool on = fourth & (t < C::padded(KB()));
         t_slot = on ? next_slot(t_slot) : t_slot;
         t_block = on ? scale_block((t >> 2) + 1) : t_block;
     };
@@ -489,7 +509,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
     constexpr bool SX4 = TM <= 4;          // a lane's scales of four steps in registers, for every X fragment
     v4f sx4[SX4 ? TM : 1];
     float sx[RING];                        // or those of the fragments that were read
-    int slot = 0, sw_at = kWScales + wn / 2 * KB * 4;
+    int slot = 0, sw_at = kWScales + wn / 2 * part_blocks * 4;
     float sw = *reinterpret_cast<const float*>(smem + sw_at);
 #pragma unroll
     for (int i = 0; i < TN; ++i) read(wf_at, i * 512, wf[i]);
@@ -505,7 +525,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 
     for (;;) {
         const Rows here = r;       // (the loads move on to the next tile before this one is done)
-        const int here_n0 = n0, here_tile = tile;
+        const int here_n0 = n0, here_tile = tile, here_part = part, blocks = KB();
         // p: the products of the X fragment before (and of the present one, where there are the registers)
         constexpr int P = TM >= 8 ? 1 : 2;
         v4f acc[TM][TN], p[P][TN];
@@ -519,22 +539,22 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 
         // Step u of a chunk, 0 .. 3 (those past the last block add nothing: their scales are zeros): a constant where four steps are unrolled, so that a stage's
         // places are too, or not, where that takes more registers than there are.
-        int steps = C::padded(KB), kt = 0;
+        int steps = C::padded(blocks), kt = 0;
         asm volatile("" : "+s"(steps));    // (nothing that the compiler knows: every unrolled step is a block of its own to it, whose order it keeps)
         auto step = [&](auto u) {
             const int STAGE = u % S * C::STAGE, NEXT = (u + 1) % S * C::STAGE, FILL = (u + S - 1) % S * C::STAGE;
             const int Q = (u + S - 1) % 4;         // the part of a chunk that goes out
-            const bool last = kt + 4 - u >= KB;    // this is the tile's last chunk
+            const bool last = kt + 4 - u >= blocks;    // this is the tile's last chunk
             const int slot_next = next_slot(slot);
-            const int sw_next_at = u < 3 ? sw_at + 4 * (u + 1) : last ? kWScales + w_side * C::w_room(KB) + wn / 2 * KB * 4 : sw_at + 16;   // (the next tile's, when the loads are there)
+            const int sw_next_at = u < 3 ? sw_at + 4 * (u + 1) : last ? kWScales + w_side * C::w_room(part_blocks) + wn / 2 * part_blocks * 4 : sw_at + 16;   // (the next tile's, when the loads are there)
             auto meet = [&]() {
                 wait_vmcnt<(EARLY ? S - 3 : S - 2) * LPS>();
                 if constexpr (!EARLY) wait_lgkmcnt0();    // (early: what was read of the stage before has been multiplied)
                 block_barrier();
             };
             if constexpr (EARLY) meet();
-            Half32 wh[OUT_F32 ? TN : 1];
-            if constexpr (OUT_F32) {
+            Half32 wh[EXACT ? TN : 1];
+            if constexpr (EXACT) {
 #pragma unroll
                 for (int i = 0; i < TN; ++i) wh[i] = to_half(wf[i]);
             }
@@ -559,7 +579,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
                     sw_next = *reinterpret_cast<const float*>(smem + sw_next_at);
                 }
                 Half32 xh;
-                if constexpr (OUT_F32) xh = to_half(xf[j % RING]);
+                if constexpr (EXACT) xh = to_half(xf[j % RING]);
 #pragma unroll
                 for (int i = 0; i < TN; ++i) {
                     v4f& to = acc[j == 0 ? TM - 1 : j - 1][i];
@@ -568,7 +588,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
                         for (int e = 0; e < 4; ++e) to[e] = fmaf(s, q[e], to[e]);
                     };
                     if constexpr (P == 1) add(p[0][i]);
-                    if constexpr (OUT_F32) p[P == 1 ? 0 : j & 1][i] = mfma_half(wh[i], xh);
+                    if constexpr (EXACT) p[P == 1 ? 0 : j & 1][i] = mfma_half(wh[i], xh);
                     else p[P == 1 ? 0 : j & 1][i] = mfma_fp8(wf[i], xf[j % RING]);
                     if constexpr (P == 2) add(p[1 - (j & 1)][i]);
                     if (j == TM - 1) read(wf_at, NEXT + i * 512, wf[i]);
@@ -584,7 +604,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
                 } else {
                     s = sx[j % RING] * sw;
                 }
-                if (u > 0) s = kt < KB ? s : 0.0f;
+                if (u > 0) s = kt < blocks ? s : 0.0f;
                 sw = sw_next;
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -638,7 +658,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
         char* const room = smem + kRoom + wave * (C::out(OUT_F32) / NW);
         const int row0 = here.begin + wm * TM * 16 + lane / PIECES, col = here_n0 + wn * 64 + lane % PIECES * EACH, have = (int)g.N - col;
         const bool inside = here.begin + (wm + 1) * TM * 16 <= here.end && here_n0 + wn * 64 + 64 <= (int)g.N;
-        Out* out = static_cast<Out*>(g.out) + (int64_t)row0 * g.N + col;
+        Out* out = static_cast<Out*>(g.out) + ((int64_t)here_part * g.rows + row0) * g.N + col;
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
 #pragma unroll
@@ -680,16 +700,54 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
     wait_vmcnt<0>();    // (loads to LDS past the last step)
 }
 
-template <bool GROUPED, bool OUT_F32, typename C>
-hipError_t launch_tile(const Fp8Args& g, hipStream_t st)
+template <bool GROUPED, bool EXACT, bool OUT_F32, bool SPLIT, typename C>
+hipError_t launch_tile(const Fp8Args& g, int parts, int part_blocks, hipStream_t st)
 {
     static LdsAttrOnce attr;
-    const int KB = (int)(g.K >> 7);
-    const hipError_t e = attr.ensure(reinterpret_cast<const void*>(fp8_tile_kernel<GROUPED, OUT_F32, C>), 163840 / C::PER_CU);
+    const hipError_t e = attr.ensure(reinterpret_cast<const void*>(fp8_tile_kernel<GROUPED, EXACT, OUT_F32, SPLIT, C>), 163840);
     if (e != hipSuccess) return e;
     const int64_t tiles_m = GROUPED ? g.rows / C::BM + std::min<int64_t>(g.experts, g.rows) : (g.rows + C::BM - 1) / C::BM, tiles_n = (g.N + C::BN - 1) / C::BN;
-    const int64_t grid = std::min<int64_t>(tiles_m * tiles_n, (int64_t)compute_units() * C::PER_CU);
-    hipLaunchKernelGGL((fp8_tile_kernel<GROUPED, OUT_F32, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(KB, OUT_F32), st, g, (int)tiles_m, (int)tiles_n);
+    const int64_t grid = std::min<int64_t>(tiles_m * tiles_n * parts, compute_units());
+    hipLaunchKernelGGL((fp8_tile_kernel<GROUPED, EXACT, OUT_F32, SPLIT, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(part_blocks, OUT_F32), st, g, (int)tiles_m, (int)tiles_n, parts,
+                       part_blocks);
+    return hipGetLastError();
+}
+
+// The parts' sums in their order.
+template <bool OUT_F32>
+__global__ __launch_bounds__(256) void fp8_join_kernel(const float* part, int parts, int64_t n, void* out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    if (i + 4 <= n && n % 4 == 0) {
+        v4f sum = *reinterpret_cast<const v4f*>(part + i);
+        for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const v4f*>(part + p * n + i);
+        if constexpr (OUT_F32) {
+            *reinterpret_cast<v4f*>(static_cast<float*>(out) + i) = sum;
+        } else {
+            typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<v2i*>(static_cast<__bf16*>(out) + i) = __builtin_bit_cast(v2i, v4b{(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]});
+        }
+    } else {
+        for (int64_t e = i; e < i + 4 && e < n; ++e) {
+            float sum = part[e];
+            for (int p = 1; p < parts; ++p) sum += part[p * n + e];
+            if constexpr (OUT_F32) static_cast<float*>(out)[e] = sum;
+            else static_cast<__bf16*>(out)[e] = (__bf16)sum;
+        }
+    }
+}
+
+// A product in parts of K on tiles of C, and their sum.
+template <bool OUT_F32, typename C>
+hipError_t launch_parts(Fp8Args g, int parts, int part_blocks, void* partial, hipStream_t st)
+{
+    void* const out = g.out;
+    g.out = partial;
+    const hipError_t e = launch_tile<false, OUT_F32, true, true, C>(g, parts, part_blocks, st);
+    if (e != hipSuccess) return e;
+    const int64_t n = g.rows * g.N;
+    hipLaunchKernelGGL(fp8_join_kernel<OUT_F32>, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, st, static_cast<const float*>(partial), parts, n, out);
     return hipGetLastError();
 }
 
@@ -708,48 +766,108 @@ hipError_t launch_stream(const Fp8Args& g, hipStream_t st)
 typedef Tile<8, 2, 4, 2> Tile256;           // 256 x 256
 typedef Tile<4, 2, 2, 4> Tile128;           // 128 x 128
 typedef Tile<2, 2, 2, 4> Tile64;            // 64 x 128
-typedef Tile<2, 4, 2, 4> TileX;            // 128 x 128, 8 waves
 
-template <bool GROUPED, bool OUT_F32, typename C>
-bool tile_takes(const Fp8Args& g)
+// How a product runs.
+struct Plan {
+    int kind = 0;              // 0 .. 3: few rows, with 16 or 32 rows and 16 or 32 columns to a tile (bit 0: columns, bit 1: rows); 4, 5, 6: tiles of 64, 128, 256 rows
+    int parts = 1, part_blocks = 0;
+};
+
+// What a kind takes, microseconds on a device of `cus` compute units, measured on 256.  Few rows: W once for every row of tiles, at what they stream with all compute
+// units at work.  Tiles: rounds of them, each a fixed part and the steps of K (fp32 sums take twice the time).  Parts add the writing, reading and launch of their sum.
+double kind_us(int kind, double rows, double tiles_m, double N, int64_t blocks, int parts, bool exact, int cus)
 {
-    const int64_t KB = g.K >> 7;
-    return KB >= 4 && KB <= C::max_blocks(OUT_F32) && !(GROUPED && g.index && g.a_rows * g.K > (int64_t)kOutside);
+    if (kind < 4) {
+        static const double rate[] = {4.3e6, 4.5e6, 3.4e6, 3.9e6};
+        const double tiles = tiles_m * std::ceil(N / (kind & 1 ? 32 : 16)), wgs = std::min(tiles, kind == 0 ? 2.0 * cus : cus);
+        return 3.2 + tiles_m * N * 128 * (double)blocks / (rate[kind] * std::min(1.0, wgs / cus) * cus / 256.0);
+    }
+    static const double fixed[] = {2.5, 4.0, 9.0}, step[] = {0.42, 0.60, 1.70}, cols[] = {128, 128, 256};
+    const int64_t steps = ((blocks + parts - 1) / parts + 3) / 4 * 4;
+    const double rounds = std::ceil(tiles_m * std::ceil(N / cols[kind - 4]) * parts / cus);
+    return 3.0 + rounds * (fixed[kind - 4] + (double)steps * step[kind - 4] * (exact ? 2 : 1)) + (parts > 1 ? 2.5 + parts * rows * N * 8 / 4e6 : 0.0);
+}
+
+constexpr int kKinds = 7;
+constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(false), Tile128::max_blocks(false), Tile256::max_blocks(false)},
+                                       {1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(true), 0, 0}};
+constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256};
+
+// The kind that takes least; in parts only where `room` bytes hold their sums.  Kinds of tiles take K from 512 on, where there is room for the scales of W; rows
+// that are gathered out of more than 4 GB are the few-row kinds' too (which is slow, but right).
+Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
+{
+    const int64_t blocks = g.K >> 7;
+    const int forced = options().fp8_variant, cus = compute_units();
+    Plan best;
+    best.part_blocks = (int)blocks;
+    if (g.index && (grouped ? g.a_rows : g.rows) * g.K > (int64_t)kOutside) return best;
+    double best_us = 1e30;
+    for (int kind = 0; kind < kKinds; ++kind) {
+        if (kind >= 4 && blocks < 4) break;
+        // rows of tiles; by expert: as if the rows were spread evenly over the experts, half a tile more to each than they fill
+        const double active = (double)std::min<int64_t>(g.experts, g.rows);
+        const double tiles_m = grouped ? active * std::max(1.0, (double)g.rows / active / kRows[kind] + 0.4) : (double)((g.rows + kRows[kind] - 1) / kRows[kind]);
+        for (int parts = 1; parts <= 16; ++parts) {
+            if (parts > 1 && (grouped || kind < 4 || kind > 5 || (size_t)parts * g.rows * g.N * 4 > room)) break;
+            const int64_t each = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
+            if (each > kMaxBlocks[out_f32][kind]) continue;
+            if (parts > 1 && (parts - 1) * each >= blocks) continue;      // (a part of nothing)
+            const double us = kind_us(kind, (double)g.rows, tiles_m, (double)g.N, blocks, parts, out_f32, cus);
+            const bool chosen = forced ? kind == (forced <= kKinds ? forced - 1 : forced <= 10 ? 4 : 5) && parts == (forced <= kKinds ? 1 : 2 << (forced - 8) % 3) : us < best_us;
+            if (chosen) {
+                best = Plan{kind, parts, (int)each};
+                best_us = us;
+            }
+        }
+    }
+    return best;
 }
 
 template <bool GROUPED, bool OUT_F32>
-hipError_t launch(const Fp8Args& g, hipStream_t st)
+hipError_t launch(const Fp8Args& g, const Plan& p, void* partial, hipStream_t st)
 {
-    const int variant = options().gemm_variant;
-    if constexpr (!OUT_F32) if (variant == 1 && tile_takes<GROUPED, OUT_F32, Tile256>(g)) return launch_tile<GROUPED, OUT_F32, Tile256>(g, st);
-    if constexpr (!OUT_F32) if (variant == 2 && tile_takes<GROUPED, OUT_F32, Tile128>(g)) return launch_tile<GROUPED, OUT_F32, Tile128>(g, st);
-    if (variant == 4 && tile_takes<GROUPED, OUT_F32, TileX>(g)) return launch_tile<GROUPED, OUT_F32, TileX>(g, st);
-    if (variant == 3 && tile_takes<GROUPED, OUT_F32, Tile64>(g)) return launch_tile<GROUPED, OUT_F32, Tile64>(g, st);
-    if (variant == 10) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 8, 4>>(g, st);
-    if (variant == 11) return launch_stream<GROUPED, OUT_F32, Stream<1, 2, 4, 5>>(g, st);
-    if (variant == 12) return launch_stream<GROUPED, OUT_F32, Stream<2, 1, 4, 5>>(g, st);
-    if (variant == 13) return launch_stream<GROUPED, OUT_F32, Stream<2, 2, 4, 3>>(g, st);
-    if (variant == 14) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 4, 4>>(g, st);
-    if (variant == 15) return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 4, 8>>(g, st);
-    if (variant == 16) return launch_stream<GROUPED, OUT_F32, Stream<2, 1, 8, 2>>(g, st);
-    if (variant == 17) return launch_stream<GROUPED, OUT_F32, Stream<1, 2, 8, 2>>(g, st);
-    return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 8, 4>>(g, st);
+    if constexpr (!GROUPED) {
+        if (p.parts > 1) {
+            if (p.kind == 4) return launch_parts<OUT_F32, Tile64>(g, p.parts, p.part_blocks, partial, st);
+            if constexpr (!OUT_F32) return launch_parts<OUT_F32, Tile128>(g, p.parts, p.part_blocks, partial, st);
+        }
+    }
+    switch (p.kind) {
+        case 1: return launch_stream<GROUPED, OUT_F32, Stream<1, 2, 4, 5>>(g, st);
+        case 2: return launch_stream<GROUPED, OUT_F32, Stream<2, 1, 4, 5>>(g, st);
+        case 3: return launch_stream<GROUPED, OUT_F32, Stream<2, 2, 4, 3>>(g, st);
+        case 4: return launch_tile<GROUPED, OUT_F32, OUT_F32, false, Tile64>(g, 1, p.part_blocks, st);
+        case 5: if constexpr (!OUT_F32) return launch_tile<GROUPED, false, false, false, Tile128>(g, 1, p.part_blocks, st); break;
+        case 6: if constexpr (!OUT_F32) return launch_tile<GROUPED, false, false, false, Tile256>(g, 1, p.part_blocks, st); break;
+        default: break;
+    }
+    return launch_stream<GROUPED, OUT_F32, Stream<1, 1, 4, 4>>(g, st);
 }
 
 }  // namespace
 
+size_t fp8_gemm_partial_bytes(int64_t M, int64_t N, int64_t K, bool out_f32)
+{
+    const Fp8Args g{nullptr, nullptr, nullptr, nullptr, nullptr, M, N, K, M, nullptr, nullptr, 1};
+    const Plan p = plan_fp8(g, false, out_f32, SIZE_MAX);
+    return p.parts > 1 ? (size_t)p.parts * M * N * 4 : 0;
+}
+
 hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
-                           hipStream_t st)
+                           void* partial, size_t room, hipStream_t st)
 {
     const Fp8Args g{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, M, N, K, M, nullptr, nullptr, 1};
-    return out_f32 ? launch<false, true>(g, st) : launch<false, false>(g, st);
+    const Plan p = plan_fp8(g, false, out_f32, room);
+    return out_f32 ? launch<false, true>(g, p, partial, st) : launch<false, false>(g, p, partial, st);
 }
 
 hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st)
 {
     const Fp8Args g{static_cast<const uint8_t*>(a), a_scales, static_cast<const uint8_t*>(w), w_scales, out, a_rows, N, K, rows, offsets, index, (int)experts};
-    return out_f32 ? launch<true, true>(g, st) : launch<true, false>(g, st);
+    const Plan p = plan_fp8(g, true, out_f32, 0);
+    return out_f32 ? launch<true, true>(g, p, nullptr, st) : launch<true, false>(g, p, nullptr, st);
 }
 
 }  // namespace fp4mr

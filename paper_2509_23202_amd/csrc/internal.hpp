@@ -14,6 +14,7 @@ namespace fp4mr {
 struct Options {
     int gemm_variant = 0;  // 0 = tile shape by the cost model, else a forced tile configuration of the GEMM kernels
     int gemm_grid = 0;     // > 0: cap on the number of persistent workgroups (a small grid walks many tiles each)
+    int fp8_variant = 0;   // 0 = by the cost model, else a forced kernel of the 8-bit products
     int sw_codec = 0;      // != 0: element and scale codecs in integer arithmetic instead of the converting instructions
 };
 Options& options();
@@ -39,6 +40,7 @@ int compute_units();
 // largest valid forced tile configuration per format (fp4_gemm rejects anything else before it launches)
 constexpr int kMaxGemmVariantMx = 18;
 constexpr int kMaxGemmVariantNv = 4;
+constexpr int kMaxFp8Variant = 13;
 // NVFP4: chosen as by itself, but without the kernel that dequantizes both operands in its waves
 constexpr int kVariantNvNoCodes = 4;
 
@@ -171,8 +173,10 @@ constexpr int64_t kFp8NormMaxK = 65536;
 hipError_t launch_fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t rows, int64_t K, float eps,
                                        void* codes, float* scales, void* residual_out, void* norm_out, hipStream_t st);
 hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes, float* scales, hipStream_t st);
+// partial: room for the sums of parts of K (fp8_gemm_partial_bytes: what the best plan takes; with less another one)
+size_t fp8_gemm_partial_bytes(int64_t M, int64_t N, int64_t K, bool out_f32);
 hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
-                           hipStream_t st);
+                           void* partial, size_t room, hipStream_t st);
 hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
 

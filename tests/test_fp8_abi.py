@@ -5,7 +5,7 @@ from pathlib import Path
 import pytest
 
 HEADER = Path(__file__).resolve().parent.parent / "include" / "fp4mr.h"
-NAMES = ("fp8_rmsnorm_quantize", "fp8_quantize", "fp8_quantize_weights", "fp8_gemm", "fp8_grouped_gemm")
+NAMES = ("fp8_rmsnorm_quantize", "fp8_quantize", "fp8_quantize_weights", "fp8_gemm", "fp8_workspace_bytes", "fp8_grouped_gemm")
 
 
 @pytest.fixture(scope="module")
@@ -55,10 +55,12 @@ def test_arguments_are_checked_before_any_launch(b):
     assert weights(w=None) == NULL and weights(codes=None) == NULL and weights(E=0) == SHAPE and weights(N=0) == SHAPE and weights(K=130) == SHAPE
     assert weights(E=1 << 16, N=1 << 24, K=1 << 14) == SHAPE and weights(flags=1) == FMT and weights(codes=fake + 1) == ALIGN
 
-    gemm = call(L.fp8_gemm, ("a", "sa", "w", "sw", "M", "N", "K", "out", "flags", "st"), dict(a=fake, sa=fake, w=fake, sw=fake, M=4, N=16, K=128, out=fake, flags=0, st=None))
+    gemm = call(L.fp8_gemm, ("a", "sa", "w", "sw", "M", "N", "K", "out", "ws", "wsz", "flags", "st"),
+                dict(a=fake, sa=fake, w=fake, sw=fake, M=4, N=16, K=128, out=fake, ws=None, wsz=0, flags=0, st=None))
     for n in ("a", "sa", "w", "sw", "out"):
         assert gemm(**{n: None}) == NULL and gemm(**{n: fake + 4}) == ALIGN, n
     assert gemm(K=64) == SHAPE and gemm(N=0) == SHAPE and gemm(M=-1) == SHAPE and gemm(N=(1 << 24) + 1) == SHAPE
+    assert gemm(K=(1 << 22) + 128) == SHAPE and gemm(M=1 << 24, N=(1 << 14) + 1) == SHAPE and gemm(ws=fake + 4, wsz=64) == ALIGN
     assert gemm(flags=b.A_LAYOUT_GEMM) == FMT and gemm(flags=1 << 20) == FMT and gemm(M=0) == 0
 
     grouped = call(L.fp8_grouped_gemm, ("a", "sa", "a_rows", "w", "sw", "off", "idx", "rows", "E", "N", "K", "out", "flags", "st"),
@@ -69,3 +71,12 @@ def test_arguments_are_checked_before_any_launch(b):
     assert grouped(idx=None) == SHAPE                                       # without an index every row of A is a row of the output
     assert grouped(a_rows=0) == SHAPE and grouped(E=0) == SHAPE and grouped(E=(1 << 16) + 1) == SHAPE and grouped(rows=-1) == SHAPE and grouped(K=100) == SHAPE
     assert grouped(flags=b.W_LAYOUT_GEMM) == FMT and grouped(rows=0, out=None) == 0
+
+
+def test_workspace(b):
+    """Whole fp32 copies of the output, where few tiles meet a long K; nothing for what is refused, has many tiles or few rows."""
+    n = b.fp8_workspace_bytes(200, 4096, 14336)
+    assert n > 0 and n % (200 * 4096 * 4) == 0 and 2 <= n // (200 * 4096 * 4) <= 16
+    assert b.fp8_workspace_bytes(4096, 4096, 4096) == 0 and b.fp8_workspace_bytes(1, 4096, 4096) == 0 and b.fp8_workspace_bytes(0, 4096, 4096) == 0
+    assert b.fp8_workspace_bytes(200, 4096, 100) == 0
+    assert b.lib.fp4_set_option(b.OPT_FP8_VARIANT, 14) == 4 and b.lib.fp4_set_option(b.OPT_FP8_VARIANT, -1) == 4
