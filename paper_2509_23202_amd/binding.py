@@ -99,6 +99,7 @@ try:
     from . import _calls
     _calls.bind(*(ctypes.cast(f, _p).value for f in (lib.fp4_rotate_quantize, lib.fp4_quantize_weights, lib.fp4_rotate_quantize_dense, lib.fp4_gemm,
                                                      lib.fp4_fused_linear, lib.fp4_w4a16_linear, lib.fp4_workspace_bytes, lib.fp4_packed_bytes)), Fp4mrError)
+    _calls.bind8(*(ctypes.cast(f, _p).value for f in (lib.fp8_rmsnorm_quantize, lib.fp8_quantize, lib.fp8_gemm, lib.fp8_workspace_bytes, lib.fp8_grouped_gemm)))
 except ImportError:
     _calls = None
 
@@ -377,6 +378,10 @@ def fp8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residua
     """codes, scales, h = Q(v) with v = h * weight / sqrt(mean(h^2) + eps) and h = bf16(x + residual), or x (then the third result is None).
     x: bf16 [M,K], rows may be apart (K % 128 == 0, K <= 65536); weight: bf16 [K]; residual: bf16 [M,K].  residual_out: where h goes (may be residual
     or x themselves, a new tensor if None); norm_out: bf16 [M,K] to receive v too."""
+    if _calls is not None and residual_out is None and codes is None and scales is None:
+        out = _calls.rmsnorm_quantize8(x, weight, eps, residual, norm_out)
+        if out is not None:
+            return out
     M, K, stride = _rows(x)
     _is_bf16(weight, K)
     empty = x.new_empty if type(x) is _Tensor else _plain_empty(x)
@@ -396,6 +401,10 @@ def fp8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residua
 
 def fp8_quantize(x, *, flags: int = 0, codes=None, scales=None):
     """codes, scales = Q(x) of bf16 activations [M,K], or with SILU_MUL of silu(x[:, :K]) * x[:, K:] of x [M, 2K]; rows may be apart, K % 128 == 0."""
+    if _calls is not None and codes is None and scales is None:
+        out = _calls.quantize8(x, flags)
+        if out is not None:
+            return out
     M, K, stride = _rows(x)
     if flags & SILU_MUL:
         assert K % 2 == 0
@@ -433,6 +442,10 @@ def _product_out(a_codes, a_scales, w_codes, w_scales, dim: int, rows: int, flag
 
 def fp8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None, workspace=None):
     """out[M,N] = A W^T (bf16, or fp32 with OUT_F32) from the codes and scales of activations [M,K] and weights [N,K]."""
+    if _calls is not None and out is None and workspace is None:
+        got = _calls.gemm8(a_codes, a_scales, w_codes, w_scales, flags)
+        if got is not None:
+            return got
     M = a_codes.shape[0]
     out, N, K = _product_out(a_codes, a_scales, w_codes, w_scales, 2, M, flags, out)
     need = fp8_workspace_bytes(M, N, K, flags)
@@ -451,6 +464,10 @@ def fp8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=None
     """Rows offsets[e] .. offsets[e+1] - 1 of out = those rows of A times the weights of expert e, w_codes [E,N,K]; offsets: int32 cuda [E+1].
     rows: int32 cuda [T], the row of A for each row of out (outside A: a row of zeros); without it out has A's rows.  Rows of out that no expert has are
     not written (a new out holds what its memory held)."""
+    if _calls is not None and out is None:
+        got = _calls.gemm8(a_codes, a_scales, w_codes, w_scales, flags, offsets, rows)
+        if got is not None:
+            return got
     E = w_codes.shape[0]
     assert offsets.is_cuda and offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.numel() == E + 1
     T = a_codes.shape[0]

@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
+#include <initializer_list>
 
 #include "fp4mr.h"
 
@@ -33,6 +34,13 @@ struct Entry {
     decltype(&fp4_workspace_bytes) workspace_bytes;
     decltype(&fp4_packed_bytes) packed_bytes;
 } entry;
+struct Entry8 {     // of the 8-bit linear layers
+    decltype(&fp8_rmsnorm_quantize) rmsnorm_quantize8;
+    decltype(&fp8_quantize) quantize8;
+    decltype(&fp8_gemm) gemm8;
+    decltype(&fp8_workspace_bytes) workspace_bytes8;
+    decltype(&fp8_grouped_gemm) grouped_gemm8;
+} entry8;
 PyObject* error;   // the binding's exception, called with a status
 
 // an argument that is a plain Python int in range
@@ -169,6 +177,142 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 8-bit linear layers
+constexpr int64_t kBlock8 = 128;
+
+// bf16 [M, any] whose rows may be apart
+bool bf16_strided(const at::Tensor& x) { return x.scalar_type() == at::kBFloat16 && x.dim() == 2 && x.stride(1) == 1; }
+int64_t row_stride(const at::Tensor& x) { return x.size(0) > 1 ? x.stride(0) : x.size(1); }
+bool bf16_like(const at::Tensor* t, int64_t rows, int64_t K) { return !t || (bf16_rows(*t) && t->size(0) == rows && t->size(1) == K); }
+
+// codes [.., n, K] and their scales, a row of them for `rows` rows of codes
+bool operand8(const at::Tensor& codes, const at::Tensor& scales, int64_t dim, int64_t rows)
+{
+    if (codes.scalar_type() != at::kFloat8_e4m3fn || scales.scalar_type() != at::kFloat || codes.dim() != dim || scales.dim() != dim || !codes.is_contiguous() || !scales.is_contiguous())
+        return false;
+    return codes.size(dim - 1) == scales.size(dim - 1) * kBlock8 && scales.size(dim - 2) == (codes.size(dim - 2) + rows - 1) / rows && (dim == 2 || codes.size(0) == scales.size(0));
+}
+
+PyObject* tuple(std::initializer_list<at::Tensor> tensors)      // (an undefined one is None)
+{
+    PyObject* const out = PyTuple_New((Py_ssize_t)tensors.size());
+    if (!out) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor& t : tensors) {
+        PyObject* const o = THPVariable_Wrap(t);
+        if (!o) {
+            Py_DECREF(out);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(out, i++, o);
+    }
+    return out;
+}
+
+// rmsnorm_quantize8(x, weight, eps, residual, norm_out): into new tensors, but for norm_out
+PyObject* rmsnorm_quantize8(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight, *residual, *norm;
+    if (n != 5 || !plain() || !tensor(args[0], x) || !tensor(args[1], weight) || !PyFloat_CheckExact(args[2]) || !tensor(args[3], residual, true) || !tensor(args[4], norm, true) ||
+        !bf16_strided(*x))
+        Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1);
+    if (M <= 0 || K <= 0 || K % kBlock8 != 0 || weight->scalar_type() != at::kBFloat16 || weight->dim() != 1 || weight->size(0) != K || !weight->is_contiguous() || !bf16_like(residual, M, K) ||
+        !bf16_like(norm, M, K))
+        Py_RETURN_NONE;
+    const at::Tensor codes = empty({M, K}, at::kFloat8_e4m3fn, *x), scales = empty({M, K / kBlock8}, at::kFloat, *x);
+    at::Tensor sum;
+    if (residual) sum = empty({M, K}, at::kBFloat16, *x);
+    const float eps = (float)PyFloat_AS_DOUBLE(args[2]);
+    const void *const px = x->data_ptr(), *const pw = weight->data_ptr();
+    void *const pr = pointer(residual), *const pn = pointer(norm), *const pc = codes.data_ptr(), *const ps = residual ? sum.data_ptr() : nullptr, *const st = stream();
+    float* const psc = static_cast<float*>(scales.data_ptr());
+    const int64_t apart = row_stride(*x);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8.rmsnorm_quantize8(px, apart, pr, pw, M, K, eps, pc, psc, ps, pn, 0, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({codes, scales, sum});
+    END_HANDLE_TH_ERRORS
+}
+
+// quantize8(x, flags)
+PyObject* quantize8(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor* x;
+    int64_t flags;
+    if (n != 2 || !plain() || !tensor(args[0], x) || !integer(args[1], flags) || (flags & ~(int64_t)FP4MR_SILU_MUL) || !bf16_strided(*x)) Py_RETURN_NONE;
+    const int64_t M = x->size(0), held = x->size(1), K = flags ? held / 2 : held;
+    if (M <= 0 || K <= 0 || K % kBlock8 != 0 || (flags && held % 2 != 0)) Py_RETURN_NONE;
+    const at::Tensor codes = empty({M, K}, at::kFloat8_e4m3fn, *x), scales = empty({M, K / kBlock8}, at::kFloat, *x);
+    const void* const px = x->data_ptr();
+    void *const pc = codes.data_ptr(), *const st = stream();
+    float* const psc = static_cast<float*>(scales.data_ptr());
+    const int64_t apart = row_stride(*x);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8.quantize8(px, apart, M, K, pc, psc, (uint32_t)flags, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({codes, scales});
+    END_HANDLE_TH_ERRORS
+}
+
+// gemm8(a_codes, a_scales, w_codes, w_scales, flags), and with two arguments more, offsets and rows (or None), the product by expert
+PyObject* gemm8(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *a, *sa, *w, *sw, *offsets = nullptr, *rows = nullptr;
+    int64_t flags;
+    const bool grouped = n == 7;
+    if ((n != 5 && !grouped) || !plain() || !tensor(args[0], a) || !tensor(args[1], sa) || !tensor(args[2], w) || !tensor(args[3], sw) || !integer(args[4], flags) ||
+        (flags & ~(int64_t)FP4MR_OUT_F32) || !operand8(*a, *sa, 2, 1) || !operand8(*w, *sw, grouped ? 3 : 2, kBlock8) || a->size(1) != w->size(-1))
+        Py_RETURN_NONE;
+    if (grouped && (!tensor(args[5], offsets) || !tensor(args[6], rows, true) || offsets->scalar_type() != at::kInt || !offsets->is_contiguous() || offsets->numel() != w->size(0) + 1 ||
+                    (rows && (rows->scalar_type() != at::kInt || rows->dim() != 1 || !rows->is_contiguous()))))
+        Py_RETURN_NONE;
+    const int64_t a_rows = a->size(0), M = rows ? rows->size(0) : a_rows, N = w->size(-2), K = w->size(-1);
+    if (M <= 0 || N <= 0 || K <= 0) Py_RETURN_NONE;
+    const at::Tensor out = empty({M, N}, flags ? at::kFloat : at::kBFloat16, *a);
+    at::Tensor workspace;
+    const size_t need = grouped ? 0 : entry8.workspace_bytes8(M, N, K, (uint32_t)flags);
+    if (need) workspace = empty({(int64_t)need}, at::kByte, *a);
+    const void *const pa = a->data_ptr(), *const pw = w->data_ptr();
+    const float *const psa = static_cast<const float*>(sa->data_ptr()), *const psw = static_cast<const float*>(sw->data_ptr());
+    const int32_t *const po = static_cast<const int32_t*>(pointer(offsets)), *const pr = static_cast<const int32_t*>(pointer(rows));
+    void *const to = out.data_ptr(), *const pws = need ? workspace.data_ptr() : nullptr, *const st = stream();
+    const int64_t experts = grouped ? w->size(0) : 1;
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    if (grouped) status = entry8.grouped_gemm8(pa, psa, a_rows, pw, psw, po, pr, M, experts, N, K, to, (uint32_t)flags, st);
+    else status = entry8.gemm8(pa, psa, pw, psw, M, N, K, to, pws, need, (uint32_t)flags, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// The addresses of the entry points of `to` in its order, from Python integers.
+template <typename E>
+bool addresses(PyObject* const* args, E& to)
+{
+    constexpr Py_ssize_t count = sizeof(E) / sizeof(void*);
+    void* p[count];
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        p[i] = PyLong_AsVoidPtr(args[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null entry point");
+            return false;
+        }
+    }
+    static_assert(sizeof(p) == sizeof(to), "one address per entry point");
+    std::memcpy(&to, p, sizeof(to));
+    return true;
+}
+
 // bind(addresses of the eight entry points, in the order of Entry, and the exception)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -177,18 +321,20 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
         PyErr_SetString(PyExc_TypeError, "bind() takes eight addresses and an exception");
         return nullptr;
     }
-    void* p[count];
-    for (Py_ssize_t i = 0; i < count; ++i) {
-        p[i] = PyLong_AsVoidPtr(args[i]);
-        if (!p[i]) {
-            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null entry point");
-            return nullptr;
-        }
-    }
-    static_assert(sizeof(p) == sizeof(entry), "one address per entry point");
-    std::memcpy(&entry, p, sizeof(entry));
+    if (!addresses(args, entry)) return nullptr;
     Py_INCREF(args[count]);
     Py_XSETREF(error, args[count]);
+    Py_RETURN_NONE;
+}
+
+// bind8(addresses of the five entry points, in the order of Entry8), behind bind()
+PyObject* bind8(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != (Py_ssize_t)(sizeof(Entry8) / sizeof(void*))) {
+        PyErr_SetString(PyExc_TypeError, "bind8() takes five addresses");
+        return nullptr;
+    }
+    if (!addresses(args, entry8)) return nullptr;
     Py_RETURN_NONE;
 }
 
@@ -196,9 +342,13 @@ template <typename F>
 PyCFunction method(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {{"bind", method(bind), METH_FASTCALL, nullptr},
+                         {"bind8", method(bind8), METH_FASTCALL, nullptr},
                          {"quantize", method(quantize), METH_FASTCALL, nullptr},
                          {"gemm", method(gemm), METH_FASTCALL, nullptr},
                          {"linear", method(linear), METH_FASTCALL, nullptr},
+                         {"rmsnorm_quantize8", method(rmsnorm_quantize8), METH_FASTCALL, nullptr},
+                         {"quantize8", method(quantize8), METH_FASTCALL, nullptr},
+                         {"gemm8", method(gemm8), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
