@@ -18,19 +18,30 @@ constexpr uint32_t kAmaxLeast = 27u << 23;   // 2^-100
 
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ void load8(const __bf16* p, float (&v)[8])
+__device__ __forceinline__ void widen8(const v4i& raw, float (&v)[8])
 {
-    const v8b t = __builtin_bit_cast(v8b, *reinterpret_cast<const v4i*>(p));
+    const v8b t = __builtin_bit_cast(v8b, raw);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
 }
 
+// STREAM: read or written once, past the caches' interest
+template <bool STREAM>
+__device__ __forceinline__ v4i load16(const __bf16* p)
+{
+    const v4i* const q = reinterpret_cast<const v4i*>(p);
+    if constexpr (STREAM) return __builtin_nontemporal_load(q);
+    else return *q;
+}
+
+template <bool STREAM>
 __device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
 {
     v8b t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = (__bf16)v[i];
-    *reinterpret_cast<v4i*>(p) = __builtin_bit_cast(v4i, t);
+    if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4i, t), reinterpret_cast<v4i*>(p));
+    else *reinterpret_cast<v4i*>(p) = __builtin_bit_cast(v4i, t);
 }
 
 __device__ __forceinline__ uint32_t amax8(const float (&v)[8])
@@ -90,10 +101,10 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantArgs a)
         const int64_t row = i / per_row, col = (i - row * per_row) * 8;
         const __bf16* x = a.x + row * a.x_stride + col;
         float v[8];
-        load8(x, v);
+        widen8(load16<true>(x), v);
         if constexpr (SILU) {
             float u[8];
-            load8(x + a.K, u);
+            widen8(load16<true>(x + a.K), u);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = silu_mul(v[j], u[j]);
         }
@@ -114,30 +125,39 @@ struct NormArgs {
     float eps;
 };
 
-// A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes.
-template <int T, int CH>
+// A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes; all of a thread's loads are on their way before the first is
+// needed.  MANY rows: the copies that are kept are stored past the caches.
+template <int T, int CH, bool RESIDUAL, bool MANY>
 __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
 {
     __shared__ float part[T / 64];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    v4i x[CH], r[CH], w[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = min((c * T + (int)threadIdx.x) * 8, a.K - 8);      // (past the row's end its last eight again)
+        x[c] = load16<false>(a.x + row * a.x_stride + col);
+        if constexpr (RESIDUAL) r[c] = load16<false>(a.residual + row * a.K + col);
+        w[c] = load16<false>(a.weight + col);
+    }
     float v[CH][8];
     float sum = 0.0f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * T + (int)threadIdx.x) * 8;
-        if (col < a.K) {
-            load8(a.x + row * a.x_stride + col, v[c]);
-            if (a.residual) {
-                float r[8];
-                load8(a.residual + row * a.K + col, r);
+        widen8(x[c], v[c]);
+        if constexpr (RESIDUAL) {
+            float f[8];
+            widen8(r[c], f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] = (float)(__bf16)(v[c][i] + r[i]);   // the stream that is kept is the one that is normed
-                store8(a.residual_out + row * a.K + col, v[c]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+            for (int i = 0; i < 8; ++i) v[c][i] = (float)(__bf16)(v[c][i] + f[i]);   // the stream that is kept is the one that is normed
+            if (col < a.K) store8<MANY>(a.residual_out + row * a.K + col, v[c]);
         }
+        float part_sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part_sum = fmaf(v[c][i], v[c][i], part_sum);
+        sum += col < a.K ? part_sum : 0.0f;
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
@@ -153,11 +173,11 @@ __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
     for (int c = 0; c < CH; ++c) {
         const int col = (c * T + (int)threadIdx.x) * 8;
         if (col < a.K) {   // (whole blocks of sixteen lanes)
-            float w[8];
-            load8(a.weight + col, w);
+            float f[8];
+            widen8(w[c], f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[i];
-            if (a.norm_out) store8(a.norm_out + row * a.K + col, v[c]);
+            for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * f[i];
+            if (a.norm_out) store8<MANY>(a.norm_out + row * a.K + col, v[c]);
             quantize8(v[c], a.codes + row * a.K + col, a.scales + row * (a.K / 128) + col / 128, lane);
         }
     }
@@ -183,7 +203,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
         if (row0 + 16 * r < a.N) {
-            load8(a.w + at + 16 * r * a.K, v[r]);
+            widen8(load16<true>(a.w + at + 16 * r * a.K), v[r]);
             m = max(m, amax8(v[r]));
         }
     }
@@ -195,14 +215,15 @@ __global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
     const float amax = __uint_as_float(max(m, kAmaxLeast)), inv = kE4m3Max / amax;
 #pragma unroll
     for (int r = 0; r < 8; ++r)
-        if (row0 + 16 * r < a.N) *reinterpret_cast<v2i*>(a.codes + at + 16 * r * a.K) = codes8(v[r], inv);
+        if (row0 + 16 * r < a.N) __builtin_nontemporal_store(codes8(v[r], inv), reinterpret_cast<v2i*>(a.codes + at + 16 * r * a.K));
     if (threadIdx.x == 0) a.scales[block] = amax / kE4m3Max;
 }
 
-template <int T, int CH>
+template <int T, int CH, bool MANY>
 hipError_t launch_norm(const NormArgs& a, hipStream_t st)
 {
-    hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
+    if (a.residual) hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, true, MANY>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
+    else hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, false, MANY>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
     return hipGetLastError();
 }
 
@@ -223,12 +244,24 @@ hipError_t launch_fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const vo
 {
     const NormArgs a{static_cast<const __bf16*>(x), static_cast<const __bf16*>(residual), static_cast<const __bf16*>(weight), static_cast<__bf16*>(residual_out),
                      static_cast<__bf16*>(norm_out), static_cast<uint8_t*>(codes), scales, x_stride, rows, (int)K, eps};
+    // Many rows: sixteen values to a thread.  Few: eight, so that a row takes the shorter.
     const int64_t n8 = K / 8;
-    if (n8 <= 64) return launch_norm<64, 1>(a, st);
-    if (n8 <= 256) return launch_norm<256, 1>(a, st);
-    if (n8 <= 1024) return launch_norm<256, 4>(a, st);
-    if (n8 <= 2048) return launch_norm<1024, 2>(a, st);
-    return launch_norm<1024, 8>(a, st);
+    if (rows > 2 * compute_units()) {
+        if (n8 <= 128) return launch_norm<64, 2, true>(a, st);
+        if (n8 <= 256) return launch_norm<128, 2, true>(a, st);
+        if (n8 <= 512) return launch_norm<256, 2, true>(a, st);
+        if (n8 <= 1024) return launch_norm<512, 2, true>(a, st);
+        if (n8 <= 2048) return launch_norm<1024, 2, true>(a, st);
+    } else {
+        if (n8 <= 64) return launch_norm<64, 1, false>(a, st);
+        if (n8 <= 128) return launch_norm<128, 1, false>(a, st);
+        if (n8 <= 256) return launch_norm<256, 1, false>(a, st);
+        if (n8 <= 512) return launch_norm<512, 1, false>(a, st);
+        if (n8 <= 1024) return launch_norm<1024, 1, false>(a, st);
+        if (n8 <= 2048) return launch_norm<1024, 2, false>(a, st);
+    }
+    if (n8 <= 4096) return launch_norm<1024, 4, false>(a, st);
+    return launch_norm<1024, 8, false>(a, st);
 }
 
 hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes, float* scales, hipStream_t st)
