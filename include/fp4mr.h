@@ -370,7 +370,8 @@ fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* st
  * with amax the block's largest |v| and every operation in binary32.  A block that holds a NaN or an infinity has a scale that is
  * not finite, and every output of a product that reads it is NaN or infinite.
  * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24, in products K <= 2^22 and M N <= 2^38.  No rows (M, or rows, of 0) is not an
- * error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.
+ * error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.  Scales, and the outputs of products, need the alignment of
+ * their elements only (an expert's part of them begins anywhere).
  *
  * fp8_rmsnorm_quantize: codes, scales = Q(v),  v = h * weight / sqrt(mean(h^2) + eps),  h = bf16(x + residual), or x.
  *   x            bf16, rows of K elements x_stride elements apart (x_stride >= K, a multiple of 8)
@@ -415,7 +416,8 @@ size_t fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, uint32_t flags);
  *                expert may have no rows.  Rows of out that no expert has are not written.
  *   index        device int32 [rows], the row of A for each row of out (so that a token's row is read by each of its experts from one
  *                place), or NULL: row t of A for row t of out, a_rows == rows.  A negative index, or one of a_rows or more, stands for a row of zeros.
- * offsets and index need 4-byte alignment only.  rows and a_rows <= 2^24, experts <= 65536.
+ * offsets and index need 4-byte alignment only.  rows and a_rows <= 2^24, experts <= 65536, experts * N <= 2^31; with an index, a_rows * K <=
+ * 0xf0000000.  Offsets that decrease are not an error that the call can see: which products the rows then hold is not defined.
  */
 fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int64_t a_rows, const void* w_codes, const float* w_scales,
                                 const int32_t* offsets, const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K,

@@ -14,11 +14,14 @@ inline bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uint
 template <typename... P>
 bool aligned16(const P*... p) { return (aligned(p, 16) && ...); }
 
-// (products: K up to 2^22, so that 256 rows are within 2^30 bytes; an output of 2^38 elements is more than the memory of any device)
-constexpr int64_t kMostK = 1 << 22, kMostOutput = 1ll << 38;
+// (products: K up to 2^22, so that 256 rows are within 2^30 bytes; an output of 2^38 elements, or 2^31 rows of weights, is more than
+// the memory of any device)
+constexpr int64_t kMostK = 1 << 22, kMostOutput = 1ll << 38, kMostWeightRows = 1ll << 31;
 
 bool shape(int64_t M, int64_t N, int64_t K) { return M >= 0 && M <= kMost && N > 0 && N <= kMost && K > 0 && K <= kMost && K % 128 == 0; }
 bool product(int64_t M, int64_t N, int64_t K) { return shape(M, N, K) && K <= kMostK && M <= kMostOutput / N; }
+
+uintptr_t element(uint32_t flags) { return flags & FP4MR_OUT_F32 ? 4 : 2; }
 
 fp4mr_status_t status(hipError_t e) { return e == hipSuccess ? FP4MR_OK : FP4MR_ERR_DEVICE; }
 
@@ -33,7 +36,7 @@ fp4mr_status_t fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void*
     if (!shape(M, 1, K) || K > kFp8NormMaxK || x_stride < K || x_stride % 8 != 0 || !(eps >= 0.0f)) return FP4MR_ERR_SHAPE;
     if (M == 0) return FP4MR_OK;
     if (!x || !weight || !codes_out || !scales_out || !residual != !residual_out) return FP4MR_ERR_NULL;
-    if (!aligned16(x, residual, weight, codes_out, scales_out, residual_out, norm_out)) return FP4MR_ERR_ALIGN;
+    if (!aligned16(x, residual, weight, codes_out, residual_out, norm_out) || !aligned(scales_out, 4)) return FP4MR_ERR_ALIGN;
     return status(launch_fp8_rmsnorm_quantize(x, x_stride, residual, weight, M, K, eps, codes_out, scales_out, residual_out, norm_out, static_cast<hipStream_t>(stream)));
 }
 
@@ -44,7 +47,7 @@ fp4mr_status_t fp8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t 
     if (!shape(M, 1, K) || x_stride < (silu ? 2 * K : K) || x_stride % 8 != 0) return FP4MR_ERR_SHAPE;
     if (M == 0) return FP4MR_OK;
     if (!x || !codes_out || !scales_out) return FP4MR_ERR_NULL;
-    if (!aligned16(x, codes_out, scales_out)) return FP4MR_ERR_ALIGN;
+    if (!aligned16(x, codes_out) || !aligned(scales_out, 4)) return FP4MR_ERR_ALIGN;
     return status(launch_fp8_quantize(x, x_stride, M, K, silu, codes_out, scales_out, static_cast<hipStream_t>(stream)));
 }
 
@@ -54,7 +57,7 @@ fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, i
     // (a workgroup per block)
     if (!shape(0, N, K) || experts <= 0 || experts > (1 << 16) || experts * ((N + 127) / 128) > 0x7fffffffll / (K / 128)) return FP4MR_ERR_SHAPE;
     if (!w || !codes_out || !scales_out) return FP4MR_ERR_NULL;
-    if (!aligned16(w, codes_out, scales_out)) return FP4MR_ERR_ALIGN;
+    if (!aligned16(w, codes_out) || !aligned(scales_out, 4)) return FP4MR_ERR_ALIGN;
     return status(launch_fp8_quantize_weights(w, experts, N, K, codes_out, scales_out, static_cast<hipStream_t>(stream)));
 }
 
@@ -65,7 +68,7 @@ fp4mr_status_t fp8_gemm(const void* a_codes, const float* a_scales, const void* 
     if (!product(M, N, K)) return FP4MR_ERR_SHAPE;
     if (M == 0) return FP4MR_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return FP4MR_ERR_NULL;
-    if (!aligned16(a_codes, a_scales, w_codes, w_scales, out, workspace)) return FP4MR_ERR_ALIGN;
+    if (!aligned16(a_codes, w_codes, workspace) || !aligned(a_scales, 4) || !aligned(w_scales, 4) || !aligned(out, element(flags))) return FP4MR_ERR_ALIGN;
     return status(launch_fp8_gemm(a_codes, a_scales, w_codes, w_scales, M, N, K, out, (flags & FP4MR_OUT_F32) != 0, workspace, workspace ? workspace_bytes : 0,
                                   static_cast<hipStream_t>(stream)));
 }
@@ -80,10 +83,12 @@ fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int6
 {
     if (flags & ~(uint32_t)FP4MR_OUT_F32) return FP4MR_ERR_FMT;
     if (!product(rows, N, K) || !shape(a_rows, N, K) || experts <= 0 || experts > (1 << 16)) return FP4MR_ERR_SHAPE;
-    if (index ? (rows > 0 && a_rows == 0) : a_rows != rows) return FP4MR_ERR_SHAPE;
+    if (index ? (rows > 0 && a_rows == 0) || a_rows > kFp8MaxGathered / K : a_rows != rows) return FP4MR_ERR_SHAPE;
+    if (experts > kMostWeightRows / N) return FP4MR_ERR_SHAPE;
     if (rows == 0) return FP4MR_OK;
     if (!a_codes || !a_scales || !w_codes || !w_scales || !offsets || !out) return FP4MR_ERR_NULL;
-    if (!aligned16(a_codes, a_scales, w_codes, w_scales, out) || !aligned(offsets, 4) || !aligned(index, 4)) return FP4MR_ERR_ALIGN;
+    if (!aligned16(a_codes, w_codes) || !aligned(a_scales, 4) || !aligned(w_scales, 4) || !aligned(out, element(flags)) || !aligned(offsets, 4) || !aligned(index, 4))
+        return FP4MR_ERR_ALIGN;
     return status(launch_fp8_grouped_gemm(a_codes, a_scales, a_rows, w_codes, w_scales, offsets, index, rows, experts, N, K, out, (flags & FP4MR_OUT_F32) != 0,
                                           static_cast<hipStream_t>(stream)));
 }

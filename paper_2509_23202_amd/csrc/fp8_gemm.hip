@@ -92,11 +92,11 @@ __device__ __forceinline__ ExpertTiles expert_tiles(const Fp8Args& g, int base, 
     return x;
 }
 
-// Tiles of R rows of all experts: tiles never span experts, and those of an expert follow one another.
-__device__ __forceinline__ int count_tiles(const Fp8Args& g, int R)
+// Tiles of R rows of all experts: tiles never span experts, and those of an expert follow one another.  Offsets that do not decrease make `most` at most.
+__device__ __forceinline__ int count_tiles(const Fp8Args& g, int R, int most)
 {
     int n = 0;
-    for (int base = 0; base < g.experts; base += 64) n += __shfl(expert_tiles(g, base, R).upto, 63);
+    for (int base = 0; base < g.experts; base += 64) n = min(n + __shfl(expert_tiles(g, base, R).upto, 63), most);
     return __builtin_amdgcn_readfirstlane(n);
 }
 
@@ -116,7 +116,7 @@ __device__ __forceinline__ Rows find_tile(const Fp8Args& g, int tile, int R)
     return Rows{0, 0, 0};
 }
 
-constexpr uint32_t kOutside = 0xf0000000u;    // an offset past every operand, to which K may be added
+constexpr uint32_t kOutside = (uint32_t)kFp8MaxGathered;    // an offset past every operand, to which K may be added
 constexpr uint32_t kPast = 0x08000000u;       // past all activations' scales (4 / 128 of kOutside), and kOutside may be added
 
 // What the pieces of a row are exchanged by: the sixteen rows of a fragment, which lie next to each other (X) or four by four, sixteen apart (W), have every
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int K = (int)g.K, KB = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
     const bool gather = GROUPED && g.index != nullptr;
-    if constexpr (GROUPED) tiles_m = count_tiles(g, 16 * TM);
+    if constexpr (GROUPED) tiles_m = count_tiles(g, 16 * TM, tiles_m);
     const int64_t ntiles = (int64_t)tiles_m * tiles_n;
     const int tile_first = (int)(ntiles * blockIdx.x / gridDim.x), tile_end = (int)(ntiles * (blockIdx.x + 1) / gridDim.x);
     if (tile_first >= tile_end) return;
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
     const int wm = wave % C::NWM, wn = wave / C::NWM;
     const int K = (int)g.K, KS = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
 
-    if constexpr (GROUPED) tiles_m = count_tiles(g, C::BM);
+    if constexpr (GROUPED) tiles_m = count_tiles(g, C::BM, tiles_m);
     const int ntiles = tiles_m * tiles_n * parts;
     int tile = blockIdx.x;
     if (tile >= ntiles) return;
@@ -722,12 +722,9 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(const float* part, int pa
     if (i + 4 <= n && n % 4 == 0) {
         v4f sum = *reinterpret_cast<const v4f*>(part + i);
         for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const v4f*>(part + p * n + i);
-        if constexpr (OUT_F32) {
-            *reinterpret_cast<v4f*>(static_cast<float*>(out) + i) = sum;
-        } else {
-            typedef __bf16 v4b __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<v2i*>(static_cast<__bf16*>(out) + i) = __builtin_bit_cast(v2i, v4b{(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]});
-        }
+        const __bf16 y[4] = {(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]};
+        if constexpr (OUT_F32) __builtin_memcpy(static_cast<float*>(out) + i, &sum, 16);      // (an output begins at any element)
+        else __builtin_memcpy(static_cast<__bf16*>(out) + i, y, 8);
     } else {
         for (int64_t e = i; e < i + 4 && e < n; ++e) {
             float sum = part[e];
@@ -793,15 +790,13 @@ constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile
                                        {1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(true), 0, 0}};
 constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256};
 
-// The kind that takes least; in parts only where `room` bytes hold their sums.  Kinds of tiles take K from 512 on, where there is room for the scales of W; rows
-// that are gathered out of more than 4 GB are the few-row kinds' too (which is slow, but right).
+// The kind that takes least; in parts only where `room` bytes hold their sums.  Kinds of tiles take K from 512 on, where there is room for the scales of W.
 Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
 {
     const int64_t blocks = g.K >> 7;
     const int forced = options().fp8_variant, cus = compute_units();
     Plan best;
     best.part_blocks = (int)blocks;
-    if (g.index && (grouped ? g.a_rows : g.rows) * g.K > (int64_t)kOutside) return best;
     double best_us = 1e30;
     for (int kind = 0; kind < kKinds; ++kind) {
         if (kind >= 4 && blocks < 4) break;

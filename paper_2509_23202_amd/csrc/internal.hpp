@@ -177,6 +177,8 @@ hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N
 size_t fp8_gemm_partial_bytes(int64_t M, int64_t N, int64_t K, bool out_f32);
 hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
                            void* partial, size_t room, hipStream_t st);
+// with an index a_rows * K <= kFp8MaxGathered: the kernels' offsets have 32 bits
+constexpr int64_t kFp8MaxGathered = 0xf0000000ll;
 hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
 

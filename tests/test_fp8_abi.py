@@ -41,15 +41,16 @@ def test_arguments_are_checked_before_any_launch(b):
     assert norm(K=65536 + 128, stride=1 << 20) == SHAPE and norm(M=(1 << 24) + 1) == SHAPE
     assert norm(eps=-1e-6) == SHAPE and norm(eps=float("nan")) == SHAPE
     assert norm(flags=1) == FMT and norm(flags=b.SILU_MUL) == FMT
-    for n in ("x", "w", "codes", "scales", "norm"):
+    for n in ("x", "w", "codes", "norm"):
         assert norm(**{n: fake + 8}) == ALIGN, n
+    assert norm(scales=fake + 2) == ALIGN
     assert norm(res=fake + 4, res_out=fake) == ALIGN and norm(res=fake, res_out=fake + 4) == ALIGN
     assert norm(M=0, x=None) == 0
 
     quant = call(L.fp8_quantize, ("x", "stride", "M", "K", "codes", "scales", "flags", "st"), dict(x=fake, stride=512, M=4, K=256, codes=fake, scales=fake, flags=0, st=None))
     assert quant(x=None) == NULL and quant(codes=None) == NULL and quant(scales=None) == NULL
     assert quant(K=64) == SHAPE and quant(stride=128) == SHAPE and quant(stride=504, flags=b.SILU_MUL) == SHAPE and quant(stride=516) == SHAPE and quant(M=-2) == SHAPE
-    assert quant(flags=b.LAYOUT_GEMM) == FMT and quant(x=fake + 2) == ALIGN and quant(scales=fake + 4) == ALIGN and quant(M=0, codes=None) == 0
+    assert quant(flags=b.LAYOUT_GEMM) == FMT and quant(x=fake + 2) == ALIGN and quant(scales=fake + 1) == ALIGN and quant(M=0, codes=None) == 0
 
     weights = call(L.fp8_quantize_weights, ("w", "E", "N", "K", "codes", "scales", "flags", "st"), dict(w=fake, E=2, N=100, K=256, codes=fake, scales=fake, flags=0, st=None))
     assert weights(w=None) == NULL and weights(codes=None) == NULL and weights(E=0) == SHAPE and weights(N=0) == SHAPE and weights(K=130) == SHAPE
@@ -58,7 +59,8 @@ def test_arguments_are_checked_before_any_launch(b):
     gemm = call(L.fp8_gemm, ("a", "sa", "w", "sw", "M", "N", "K", "out", "ws", "wsz", "flags", "st"),
                 dict(a=fake, sa=fake, w=fake, sw=fake, M=4, N=16, K=128, out=fake, ws=None, wsz=0, flags=0, st=None))
     for n in ("a", "sa", "w", "sw", "out"):
-        assert gemm(**{n: None}) == NULL and gemm(**{n: fake + 4}) == ALIGN, n
+        assert gemm(**{n: None}) == NULL and gemm(**{n: fake + (1 if n == "out" else 2)}) == ALIGN, n
+    assert gemm(a=fake + 8) == ALIGN and gemm(w=fake + 4) == ALIGN and gemm(out=fake + 2, flags=b.OUT_F32) == ALIGN
     assert gemm(K=64) == SHAPE and gemm(N=0) == SHAPE and gemm(M=-1) == SHAPE and gemm(N=(1 << 24) + 1) == SHAPE
     assert gemm(K=(1 << 22) + 128) == SHAPE and gemm(M=1 << 24, N=(1 << 14) + 1) == SHAPE and gemm(ws=fake + 4, wsz=64) == ALIGN
     assert gemm(flags=b.A_LAYOUT_GEMM) == FMT and gemm(flags=1 << 20) == FMT and gemm(M=0) == 0
@@ -66,10 +68,12 @@ def test_arguments_are_checked_before_any_launch(b):
     grouped = call(L.fp8_grouped_gemm, ("a", "sa", "a_rows", "w", "sw", "off", "idx", "rows", "E", "N", "K", "out", "flags", "st"),
                    dict(a=fake, sa=fake, a_rows=4, w=fake, sw=fake, off=fake, idx=fake, rows=8, E=2, N=16, K=128, out=fake, flags=0, st=None))
     for n in ("a", "sa", "w", "sw", "out"):
-        assert grouped(**{n: None}) == NULL and grouped(**{n: fake + 4}) == ALIGN, n
+        assert grouped(**{n: None}) == NULL and grouped(**{n: fake + (1 if n == "out" else 2)}) == ALIGN, n
+    assert grouped(a=fake + 8) == ALIGN and grouped(w=fake + 4) == ALIGN
     assert grouped(off=None) == NULL and grouped(off=fake + 2) == ALIGN and grouped(idx=fake + 1) == ALIGN
     assert grouped(idx=None) == SHAPE                                       # without an index every row of A is a row of the output
     assert grouped(a_rows=0) == SHAPE and grouped(E=0) == SHAPE and grouped(E=(1 << 16) + 1) == SHAPE and grouped(rows=-1) == SHAPE and grouped(K=100) == SHAPE
+    assert grouped(a_rows=1 << 20, K=4096) == SHAPE and grouped(E=1 << 16, N=1 << 16) == SHAPE      # gathered rows' offsets have 32 bits; weights beyond any memory
     assert grouped(flags=b.W_LAYOUT_GEMM) == FMT and grouped(rows=0, out=None) == 0
 
 

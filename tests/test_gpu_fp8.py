@@ -241,6 +241,80 @@ def test_grouped_rows_of_no_expert_and_indexes_outside(fp4, T, counts):
             R.check_product(out[rows], A[index[rows].cpu().numpy()], R.values(w[e], sw[e], 128), K)
 
 
+KERNELS = list(range(1, 8))      # few rows (1 to 4), tiles of 64, 128 and 256 rows
+
+
+@pytest.fixture
+def forced(fp4):
+    """Every product on one kernel, whatever the library would choose."""
+    yield lambda kernel: fp4.set_option(fp4.OPT_FP8_VARIANT, kernel)
+    fp4.set_option(fp4.OPT_FP8_VARIANT, 0)
+
+
+@pytest.mark.parametrize("kernel", KERNELS + list(range(8, 14)))
+@pytest.mark.parametrize("M,N,K", [(1, 16, 128), (5, 129, 512), (33, 136, 640), (70, 300, 1152), (260, 520, 2176), (2100, 1100, 640)])
+def test_gemm_on_every_kernel(fp4, forced, kernel, M, N, K):
+    """Each kernel on sizes that it would not be chosen for too; 8 to 13: two, four and eight parts of K."""
+    say(f"kernel {kernel} M={M} N={N} K={K}")
+    forced(kernel)
+    (a, sa), (w, sw) = R.operand(M, K, M), R.operand(N, K, N, 128, 0.01)
+    ops = [R.around(t, 0x7f if t.dtype != torch.float32 else 0xff) for t in (a, sa, w, sw)]
+    room = torch.full((16 * M * N * 4,), 0xff, dtype=torch.uint8, device="cuda")
+    out = fp4.fp8_gemm(*ops, workspace=room)
+    R.check_product(out, R.values(a, sa), R.values(w, sw, 128), K)
+    assert torch.equal(out, fp4.fp8_gemm(a, sa, w, sw, workspace=room))
+
+
+@pytest.mark.parametrize("kernel", KERNELS + [9, 12])
+@pytest.mark.parametrize("f32", [False, True])
+def test_scales_and_outputs_at_any_element(fp4, forced, kernel, f32):
+    """A part of a tensor of scales, or of an output with an odd number of columns, begins where it begins."""
+    forced(kernel)
+    M, N, K = 40, 131, 640
+    (a, sa), (w, sw) = R.operand(M, K, 1), R.operand(N, K, 2, 128, 0.01)
+    shifted = lambda t, by: torch.cat([torch.full((by,), float("nan"), device="cuda"), t.reshape(-1)])[by:].view(t.shape)
+    whole = torch.full((M + 2, N), 7.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    flags, room = fp4.OUT_F32 if f32 else 0, torch.empty(8 * M * N * 4, dtype=torch.uint8, device="cuda")
+    fp4.fp8_gemm(a, shifted(sa, 1), w, shifted(sw, 3), flags=flags, out=whole[1: M + 1], workspace=room)
+    R.check_product(whole[1: M + 1], R.values(a, sa), R.values(w, sw, 128), K)
+    assert (whole[[0, M + 1]] == 7.0).all()
+    whole.fill_(7.0)
+    fp4.fp8_grouped_gemm(a, shifted(sa, 2), w[None], shifted(sw, 1)[None], torch.tensor([9, 0, M], dtype=torch.int32, device="cuda")[1:], flags=flags, out=whole[1: M + 1])
+    R.check_product(whole[1: M + 1], R.values(a, sa), R.values(w, sw, 128), K)
+    assert (whole[[0, M + 1]] == 7.0).all()
+
+
+@pytest.mark.parametrize("kernel", [6, 7])
+def test_a_workgroup_walks_several_tiles(fp4, forced, kernel):
+    """More tiles than compute units, of whole and partial rows and columns, and a K that is not a multiple of four blocks."""
+    forced(kernel)
+    M, N, K = 4200, 4440, 896
+    (a, sa), (w, sw) = R.operand(M, K, 1), R.operand(N, K, 2, 128, 0.01)
+    out = fp4.fp8_gemm(a, sa, w, sw)
+    rows = np.r_[0:70, 250:260, 2040:2100, 4090:4200]
+    R.check_product(out[rows], R.values(a, sa)[rows], R.values(w, sw, 128), K)
+    cols = np.r_[0:20, 250:260, 4090:4110, 4430:4440]
+    R.check_product(out[:, cols].contiguous(), R.values(a, sa), R.values(w, sw, 128)[cols], K)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_grouped_on_every_kernel(fp4, forced, kernel):
+    """Experts of many sizes, empty ones among them, more tiles than compute units for the smaller tiles; rows in order, and gathered."""
+    forced(kernel)
+    counts = [700, 0, 3, 129, 0, 1100, 64, 257, 1, 400]
+    for gather in (None, 333):
+        say(f"grouped kernel {kernel} gather={gather}")
+        grouped(fp4, counts, 1100, 640, kernel, gather)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_a_k_that_only_the_few_row_kernels_take(fp4, f32):
+    M, N, K = 200, 40, 262144
+    (a, sa), (w, sw) = R.operand(M, K, 5), R.operand(N, K, 6, 128, 0.01)
+    out = fp4.fp8_gemm(a, sa, w, sw, flags=fp4.OUT_F32 if f32 else 0)
+    R.check_product(out, R.values(a, sa), R.values(w, sw, 128), K)
+
+
 def test_grouped_offsets_are_kept_within_the_rows(fp4):
     """Offsets below 0 and beyond the rows count as 0 and as the number of rows."""
     K, N, T = 256, 80, 50
@@ -250,6 +324,20 @@ def test_grouped_offsets_are_kept_within_the_rows(fp4):
     out = fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor([-5, 20, 30, 1000], dtype=torch.int32, device="cuda"))
     ref = fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor([0, 20, 30, 50], dtype=torch.int32, device="cuda"))
     assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("offsets", [[30, 10, 40, 5], [0, 50, 50, 20], [0, 0, 0, 0], [-2 ** 31, 2 ** 31 - 1, 0, 50]])
+def test_grouped_offsets_that_decrease_stay_within_the_rows(fp4, offsets):
+    """Not what the call is for, but nothing beside the output's rows is written, and rows that one expert alone has are its products."""
+    K, N, T = 640, 200, 50
+    a, sa = R.operand(T, K, 5)
+    w, sw = R.operand(3 * 256, K, 2, 128, 0.01)
+    w, sw = w.view(torch.uint8).view(3, 256, K)[:, :N].contiguous().view(torch.float8_e4m3fn), sw.view(3, 2, K // 128)
+    room = torch.full((T * N * 2 + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+    out = room[32768: -32768].view(torch.bfloat16).view(T, N)
+    fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor(offsets, dtype=torch.int32, device="cuda"), out=out)
+    torch.cuda.synchronize()
+    assert (room[:32768] == 0x5a).all() and (room[-32768:] == 0x5a).all()
 
 
 def test_no_rows(fp4):
