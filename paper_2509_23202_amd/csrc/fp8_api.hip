@@ -54,8 +54,8 @@ fp4mr_status_t fp8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t 
 fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes_out, float* scales_out, uint32_t flags, void* stream)
 {
     if (flags) return FP4MR_ERR_FMT;
-    // (a workgroup per block)
-    if (!shape(0, N, K) || experts <= 0 || experts > (1 << 16) || experts * ((N + 127) / 128) > 0x7fffffffll / (K / 128)) return FP4MR_ERR_SHAPE;
+    // (a workgroup of 256 threads per block, fewer than 2^32 threads: 2^24 blocks are more than the memory of any device)
+    if (!shape(0, N, K) || experts <= 0 || experts > (1 << 16) || experts * ((N + 127) / 128) >= (1 << 24) / (K / 128)) return FP4MR_ERR_SHAPE;
     if (!w || !codes_out || !scales_out) return FP4MR_ERR_NULL;
     if (!aligned16(w, codes_out) || !aligned(scales_out, 4)) return FP4MR_ERR_ALIGN;
     return status(launch_fp8_quantize_weights(w, experts, N, K, codes_out, scales_out, static_cast<hipStream_t>(stream)));

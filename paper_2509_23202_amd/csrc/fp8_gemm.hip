@@ -790,6 +790,8 @@ constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile
                                        {1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(true), 0, 0}};
 constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256};
 
+constexpr int64_t kMostJoined = 1 << 30;     // elements of an output that is joined from parts, four to a thread
+
 // The kind that takes least; in parts only where `room` bytes hold their sums.  Kinds of tiles take K from 512 on, where there is room for the scales of W.
 Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
 {
@@ -804,7 +806,7 @@ Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
         const double active = (double)std::min<int64_t>(g.experts, g.rows);
         const double tiles_m = grouped ? active * std::max(1.0, (double)g.rows / active / kRows[kind] + 0.4) : (double)((g.rows + kRows[kind] - 1) / kRows[kind]);
         for (int parts = 1; parts <= 16; ++parts) {
-            if (parts > 1 && (grouped || kind < 4 || kind > 5 || (size_t)parts * g.rows * g.N * 4 > room)) break;
+            if (parts > 1 && (grouped || kind < 4 || kind > 5 || g.rows * g.N > kMostJoined || (size_t)parts * g.rows * g.N * 4 > room)) break;
             const int64_t each = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
             if (each > kMaxBlocks[out_f32][kind]) continue;
             if (parts > 1 && (parts - 1) * each >= blocks) continue;      // (a part of nothing)

@@ -219,12 +219,28 @@ __global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
     if (threadIdx.x == 0) a.scales[block] = amax / kE4m3Max;
 }
 
+// (a launch takes fewer than 2^32 threads: very many rows in several)
+constexpr int64_t kNormRows = 1 << 21;
+
 template <int T, int CH, bool MANY>
-hipError_t launch_norm(const NormArgs& a, hipStream_t st)
+hipError_t launch_norm(NormArgs a, hipStream_t st)
 {
-    if (a.residual) hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, true, MANY>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
-    else hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, false, MANY>), dim3((unsigned)a.rows), dim3(T), 0, st, a);
-    return hipGetLastError();
+    for (int64_t left = a.rows; left > 0; left -= kNormRows) {
+        const dim3 grid((unsigned)(left < kNormRows ? left : kNormRows));
+        if (a.residual) hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, true, MANY>), grid, dim3(T), 0, st, a);
+        else hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, false, MANY>), grid, dim3(T), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.x += kNormRows * a.x_stride;
+        if (a.residual) {
+            a.residual += kNormRows * a.K;
+            a.residual_out += kNormRows * a.K;
+        }
+        if (a.norm_out) a.norm_out += kNormRows * a.K;
+        a.codes += kNormRows * a.K;
+        a.scales += kNormRows * (a.K / 128);
+    }
+    return hipSuccess;
 }
 
 }  // namespace

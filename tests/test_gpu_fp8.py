@@ -137,6 +137,21 @@ def test_rmsnorm_in_place_and_of_a_row_of_zeros(fp4):
     assert (ref[0].view(torch.uint8)[4] == 0).all() and torch.isfinite(ref[1]).all()
 
 
+def test_rmsnorm_of_more_rows_than_a_launch_has(fp4):
+    K, first = 128, 1 << 21
+    rows = first + 600
+    torch.manual_seed(5)
+    x, r = (torch.randn(rows, K, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w = torch.randn(K, device="cuda").to(torch.bfloat16)
+    norm = torch.empty_like(x)
+    got = fp4.fp8_rmsnorm_quantize(x, w, 1e-5, residual=r, norm_out=norm) + (norm,)
+    for part in (slice(0, first), slice(first, rows)):       # (600 rows take the kernel of many rows too: the same bits)
+        n = torch.empty_like(x[part])
+        want = fp4.fp8_rmsnorm_quantize(x[part], w, 1e-5, residual=r[part], norm_out=n) + (n,)
+        for g, e in zip(got, want):
+            assert torch.equal(g[part].view(torch.uint8), e.view(torch.uint8))
+
+
 @pytest.mark.parametrize("shape", [(1, 128), (127, 256), (128, 128), (129, 384), (300, 1152), (1, 1, 128), (3, 200, 256), (5, 129, 128)])
 def test_quantize_weights(fp4, shape):
     say(f"weights {shape}")
