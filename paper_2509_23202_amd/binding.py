@@ -99,7 +99,8 @@ try:
     from . import _calls
     _calls.bind(*(ctypes.cast(f, _p).value for f in (lib.fp4_rotate_quantize, lib.fp4_quantize_weights, lib.fp4_rotate_quantize_dense, lib.fp4_gemm,
                                                      lib.fp4_fused_linear, lib.fp4_w4a16_linear, lib.fp4_workspace_bytes, lib.fp4_packed_bytes)), Fp4mrError)
-    _calls.bind8(*(ctypes.cast(f, _p).value for f in (lib.fp8_rmsnorm_quantize, lib.fp8_quantize, lib.fp8_gemm, lib.fp8_workspace_bytes, lib.fp8_grouped_gemm)))
+    _calls.bind8(*(ctypes.cast(f, _p).value for f in (lib.fp8_rmsnorm_quantize, lib.fp8_quantize, lib.fp8_quantize_weights, lib.fp8_gemm, lib.fp8_workspace_bytes,
+                                                       lib.fp8_grouped_gemm)))
 except ImportError:
     _calls = None
 
@@ -416,6 +417,10 @@ def fp8_quantize(x, *, flags: int = 0, codes=None, scales=None):
 
 def fp8_quantize_weights(w, *, codes=None, scales=None):
     """codes, scales = Q(w) of bf16 weights [N,K], or of experts [E,N,K]: a scale per 128 x 128 block."""
+    if _calls is not None and codes is None and scales is None:
+        out = _calls.quantize_weights8(w)
+        if out is not None:
+            return out
     assert w.is_cuda and w.dim() in (2, 3) and w.dtype == torch.bfloat16 and w.is_contiguous()
     N, K = w.shape[-2:]
     shape = (*w.shape[:-2], -(-N // FP8_BLOCK), K // FP8_BLOCK)

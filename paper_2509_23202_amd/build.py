@@ -65,7 +65,7 @@ def _build_calls() -> None:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", str(HERE.parent / "include"),
            "-isystem", str(t / "include"), "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"],
-           str(CSRC / "calls.cpp"), "-o", str(tmp), "-L", str(t / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+           str(CSRC / "calls.cpp"), "-o", str(tmp), "-L", str(t / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("g++ failed for calls.cpp:\n" + r.stderr)

@@ -10,7 +10,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -37,6 +39,7 @@ struct Entry {
 struct Entry8 {     // of the 8-bit linear layers
     decltype(&fp8_rmsnorm_quantize) rmsnorm_quantize8;
     decltype(&fp8_quantize) quantize8;
+    decltype(&fp8_quantize_weights) quantize_weights8;
     decltype(&fp8_gemm) gemm8;
     decltype(&fp8_workspace_bytes) workspace_bytes8;
     decltype(&fp8_grouped_gemm) grouped_gemm8;
@@ -66,14 +69,16 @@ bool bf16_rows(const at::Tensor& x) { return x.scalar_type() == at::kBFloat16 &&
 
 void* pointer(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 
+// (not through the dispatcher, which takes 0.4 us for it: plain() has seen that nobody listens there, and where new memory is to be filled that is its work)
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like)
 {
+    if (!at::globalContext().deterministicAlgorithms()) return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
     return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
 }
 
 void* stream() { return c10::hip::getCurrentHIPStream(c10::hip::current_device()).stream(); }
 
-bool plain() { return !at::impl::torch_function_mode_enabled(); }
+bool plain() { return !at::impl::torch_function_mode_enabled() && !c10::impl::TorchDispatchModeTLS::any_modes_set(); }
 
 // what a call returns whose status is not FP4MR_OK
 PyObject* refused(fp4mr_status_t status)
@@ -261,6 +266,28 @@ PyObject* quantize8(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// quantize_weights8(w)
+PyObject* quantize_weights8(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor* w;
+    if (n != 1 || !plain() || !tensor(args[0], w) || w->scalar_type() != at::kBFloat16 || !w->is_contiguous() || (w->dim() != 2 && w->dim() != 3)) Py_RETURN_NONE;
+    const int64_t experts = w->dim() == 3 ? w->size(0) : 1, N = w->size(-2), K = w->size(-1), blocks = (N + kBlock8 - 1) / kBlock8;
+    if (experts <= 0 || N <= 0 || K <= 0 || K % kBlock8 != 0) Py_RETURN_NONE;
+    const at::Tensor codes = empty(w->sizes(), at::kFloat8_e4m3fn, *w);
+    const at::Tensor scales = w->dim() == 3 ? empty({experts, blocks, K / kBlock8}, at::kFloat, *w) : empty({blocks, K / kBlock8}, at::kFloat, *w);
+    const void* const pw = w->data_ptr();
+    void *const pc = codes.data_ptr(), *const st = stream();
+    float* const psc = static_cast<float*>(scales.data_ptr());
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8.quantize_weights8(pw, experts, N, K, pc, psc, 0, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({codes, scales});
+    END_HANDLE_TH_ERRORS
+}
+
 // gemm8(a_codes, a_scales, w_codes, w_scales, flags), and with two arguments more, offsets and rows (or None), the product by expert
 PyObject* gemm8(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -327,11 +354,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-// bind8(addresses of the five entry points, in the order of Entry8), behind bind()
+// bind8(addresses of the six entry points, in the order of Entry8), behind bind()
 PyObject* bind8(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     if (n != (Py_ssize_t)(sizeof(Entry8) / sizeof(void*))) {
-        PyErr_SetString(PyExc_TypeError, "bind8() takes five addresses");
+        PyErr_SetString(PyExc_TypeError, "bind8() takes six addresses");
         return nullptr;
     }
     if (!addresses(args, entry8)) return nullptr;
@@ -348,6 +375,7 @@ PyMethodDef methods[] = {{"bind", method(bind), METH_FASTCALL, nullptr},
                          {"linear", method(linear), METH_FASTCALL, nullptr},
                          {"rmsnorm_quantize8", method(rmsnorm_quantize8), METH_FASTCALL, nullptr},
                          {"quantize8", method(quantize8), METH_FASTCALL, nullptr},
+                         {"quantize_weights8", method(quantize_weights8), METH_FASTCALL, nullptr},
                          {"gemm8", method(gemm8), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -423,6 +423,35 @@ def test_streams_and_graphs(fp4):
             assert float(got[1].float().abs().sum()) > 0
 
 
+def test_modes_see_the_outputs_made_and_new_memory_is_filled_where_asked_for(fp4):
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Seen(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.empties = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.empties += "empty" in str(func)
+            return func(*args, **(kwargs or {}))
+
+    x, w = bf16(3, 256, 21, loud=False), bf16(130, 256, 22, loud=False)
+    plain = fp4.fp8_quantize(x) + fp4.fp8_quantize_weights(w)
+    with Seen() as seen:
+        watched = fp4.fp8_quantize(x) + fp4.fp8_quantize_weights(w)
+    assert seen.empties >= 4
+    for a, b in zip(plain, watched):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+    was = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)
+    try:      # (row 2 is nobody's)
+        y = fp4.fp8_grouped_gemm(*plain[:2], plain[2][None], plain[3][None], torch.tensor([0, 2], dtype=torch.int32, device="cuda"))
+    finally:
+        torch.use_deterministic_algorithms(was)
+    assert torch.isnan(y[2]).all() and torch.isfinite(y[:2]).all()
+
+
 def test_refusals_of_the_binding(fp4):
     (a, sa), (w, sw) = R.operand(4, 256, 1), R.operand(32, 256, 2, 128)
     x = bf16(4, 256, 3)
