@@ -77,43 +77,46 @@ struct ExpertTiles {
 };
 __device__ __forceinline__ ExpertTiles expert_tiles(const Fp8Args& g, int base, int R)
 {
-    const int lane = threadIdx.x & 63, T = (int)g.rows, e = base + lane;
-    ExpertTiles x{0, 0, 0};
-    if (e < g.experts) {
-        x.lo = min(max(g.offsets[e], 0), T);
-        x.hi = min(max(g.offsets[e + 1], x.lo), T);
-    }
-    x.upto = (x.hi - x.lo + R - 1) / R;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int t = __shfl_up(x.upto, d);
-        if (lane >= d) x.upto += t;
-    }
+    const int e = base + ((int)threadIdx.x & 63), at = min(e, g.experts - 1), T = (int)g.rows;
+    const int begin = g.offsets[at], end = g.offsets[at + 1];
+    ExpertTiles x;
+    x.lo = min(max(begin, 0), T);
+    x.hi = min(max(end, x.lo), T);
+    int n = e < g.experts ? (x.hi - x.lo + R - 1) / R : 0;
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8: the sum within sixteen lanes
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);    // row_bcast 15 to the second and fourth sixteen, row_bcast 31 to the second half
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
+    x.upto = n;
     return x;
 }
 
 // Tiles of R rows of all experts: tiles never span experts, and those of an expert follow one another.  Offsets that do not decrease make `most` at most.
-__device__ __forceinline__ int count_tiles(const Fp8Args& g, int R, int most)
+// first: of the first 64 experts.
+__device__ __forceinline__ int count_tiles(const Fp8Args& g, const ExpertTiles& first, int R, int most)
 {
-    int n = 0;
-    for (int base = 0; base < g.experts; base += 64) n = min(n + __shfl(expert_tiles(g, base, R).upto, 63), most);
-    return __builtin_amdgcn_readfirstlane(n);
+    int n = min(__builtin_amdgcn_readlane(first.upto, 63), most);
+    for (int base = 64; base < g.experts; base += 64) n = min(n + __builtin_amdgcn_readlane(expert_tiles(g, base, R).upto, 63), most);
+    return n;
 }
 
-__device__ __forceinline__ Rows find_tile(const Fp8Args& g, int tile, int R)
+__device__ __forceinline__ Rows find_tile(const Fp8Args& g, const ExpertTiles& first, int tile, int R)
 {
-    int before = 0;
-    for (int base = 0; base < g.experts; base += 64) {
-        const ExpertTiles x = expert_tiles(g, base, R);
+    ExpertTiles x = first;
+    for (int base = 0, before = 0;;) {
         const uint64_t here = __ballot(tile < before + x.upto);
         if (here) {
-            const int l = __builtin_ctzll(here), earlier = l ? __shfl(x.upto, l - 1) : 0;
-            const int first = __shfl(x.lo, l) + (tile - before - earlier) * R;
-            return Rows{__builtin_amdgcn_readfirstlane(base + l), __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(min(first + R, __shfl(x.hi, l)))};
+            const int l = __builtin_ctzll(here), earlier = l ? __builtin_amdgcn_readlane(x.upto, l - 1) : 0;
+            const int begin = __builtin_amdgcn_readlane(x.lo, l) + (tile - before - earlier) * R;
+            return Rows{base + l, begin, min(begin + R, __builtin_amdgcn_readlane(x.hi, l))};
         }
-        before += __shfl(x.upto, 63);
+        before += __builtin_amdgcn_readlane(x.upto, 63);
+        base += 64;
+        if (base >= g.experts) return Rows{0, 0, 0};
+        x = expert_tiles(g, base, R);
     }
-    return Rows{0, 0, 0};
 }
 
 constexpr uint32_t kOutside = (uint32_t)kFp8MaxGathered;    // an offset past every operand, to which K may be added
@@ -169,7 +172,11 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int K = (int)g.K, KB = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
     const bool gather = GROUPED && g.index != nullptr;
-    if constexpr (GROUPED) tiles_m = count_tiles(g, 16 * TM, tiles_m);
+    ExpertTiles experts{0, 0, 0};
+    if constexpr (GROUPED) {
+        experts = expert_tiles(g, 0, 16 * TM);
+        tiles_m = count_tiles(g, experts, 16 * TM, tiles_m);
+    }
     const int64_t ntiles = (int64_t)tiles_m * tiles_n;
     const int tile_first = (int)(ntiles * blockIdx.x / gridDim.x), tile_end = (int)(ntiles * (blockIdx.x + 1) / gridDim.x);
     if (tile_first >= tile_end) return;
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
         n0 = (tile - tm * tiles_n) * 16 * TN;
         if (tm != at_m) {
             at_m = tm;
-            if constexpr (GROUPED) r = find_tile(g, tm, 16 * TM);
+            if constexpr (GROUPED) r = find_tile(g, experts, tm, 16 * TM);
             else r = Rows{0, tm * 16 * TM, min((tm + 1) * 16 * TM, (int)g.rows)};
             const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;
             rx = make_rsrc(g.a + x0 * K, x_rows * K);
@@ -234,6 +241,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
         }
     };
     locate(tile_first);
+    const Rows r_first = r;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) issue();
 
@@ -241,8 +249,8 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
     const int l16 = lane & 15, f_at = l16 * 128 + ((lane >> 4) ^ x_key(l16)) * 16;
     int slot = 0;
     // what the tile that is multiplied has; the loads may be a tile or more ahead
-    Rows mine{0, 0, 0};
-    int mine_m = -1;
+    Rows mine = r_first;
+    int mine_m = tile_first / tiles_n;
     for (int tile = tile_first; tile < tile_end; ++tile) {
         v4f acc[TM][TN];
 #pragma unroll
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
         const int tm = tile / tiles_n, col0 = (tile - tm * tiles_n) * 16 * TN;
         if (tm != mine_m) {
             mine_m = tm;
-            if constexpr (GROUPED) mine = find_tile(g, tm, 16 * TM);
+            if constexpr (GROUPED) mine = tm == at_m ? r : find_tile(g, experts, tm, 16 * TM);
             else mine = Rows{0, tm * 16 * TM, min((tm + 1) * 16 * TM, (int)g.rows)};
         }
         for (int q = wave; q < TM * TN; q += WAVES) {
@@ -381,7 +389,12 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
     const int wm = wave % C::NWM, wn = wave / C::NWM;
     const int K = (int)g.K, KS = K >> 7, blocks_n = (int)((g.N + 127) >> 7);
 
-    if constexpr (GROUPED) tiles_m = count_tiles(g, C::BM, tiles_m);
+    constexpr bool KEEP = !C::ROLLED;      // (those have the registers)
+    ExpertTiles experts{0, 0, 0};
+    if constexpr (GROUPED) {
+        experts = expert_tiles(g, 0, C::BM);
+        tiles_m = count_tiles(g, experts, C::BM, tiles_m);
+    }
     const int ntiles = tiles_m * tiles_n * parts;
     int tile = blockIdx.x;
     if (tile >= ntiles) return;
@@ -425,7 +438,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
             part_k0 = part * part_blocks;
             part_n = min(part_blocks, KS - part_k0);
         }
-        if constexpr (GROUPED) r = find_tile(g, tm, C::BM);
+        if constexpr (GROUPED) r = find_tile(g, KEEP ? experts : expert_tiles(g, 0, C::BM), tm, C::BM);
         else r = Rows{0, tm * C::BM, min((tm + 1) * C::BM, (int)g.rows)};
         n0 = tn * C::BN;
         const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;

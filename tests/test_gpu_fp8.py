@@ -322,6 +322,14 @@ def test_grouped_on_every_kernel(fp4, forced, kernel):
         grouped(fp4, counts, 1100, 640, kernel, gather)
 
 
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_grouped_of_many_experts_on_every_kernel(fp4, forced, kernel):
+    """Tiles that are found behind the first 64 experts, and behind the first 128."""
+    forced(kernel)
+    counts = [0] * 30 + [3, 70] + [0] * 31 + [5] + [0] * 10 + [1, 0, 40] + [0] * 60 + [2, 0, 33, 0]
+    grouped(fp4, counts, 72, 512, kernel)
+
+
 @pytest.mark.parametrize("f32", [False, True])
 def test_a_k_that_only_the_few_row_kernels_take(fp4, f32):
     M, N, K = 200, 40, 262144
