@@ -25,7 +25,7 @@ __device__ __forceinline__ void widen8(const v4i& raw, float (&v)[8])
     for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
 }
 
-// STREAM: read or written once, past the caches' interest
+// STREAM: read once, past the caches' interest
 template <bool STREAM>
 __device__ __forceinline__ v4i load16(const __bf16* p)
 {
@@ -34,14 +34,12 @@ __device__ __forceinline__ v4i load16(const __bf16* p)
     else return *q;
 }
 
-template <bool STREAM>
 __device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
 {
     v8b t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = (__bf16)v[i];
-    if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4i, t), reinterpret_cast<v4i*>(p));
-    else *reinterpret_cast<v4i*>(p) = __builtin_bit_cast(v4i, t);
+    __builtin_nontemporal_store(__builtin_bit_cast(v4i, t), reinterpret_cast<v4i*>(p));
 }
 
 __device__ __forceinline__ uint32_t amax8(const float (&v)[8])
@@ -92,7 +90,8 @@ struct QuantArgs {
     float* scales;
 };
 
-// Sixteen lanes to a block of 128, in the order of the outputs.
+// Sixteen lanes to a block of 128, in the order of the outputs: 16-byte loads, a maximum in four lane exchanges, whole lines of codes.  Memory bounds it: gated 4096 x 14336 takes 47 us,
+// 6.3 TB/s, what a copy reaches; 33 x 14336 takes 2.8, a launch's.  (Loads past the caches: an input is read once.)
 template <bool SILU>
 __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantArgs a)
 {
@@ -125,9 +124,11 @@ struct NormArgs {
     float eps;
 };
 
-// A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes; all of a thread's loads are on their way before the first is
-// needed.  MANY rows: the copies that are kept are stored past the caches.
-template <int T, int CH, bool RESIDUAL, bool MANY>
+// A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes, so that a row is read once; all of a thread's loads are on
+// their way before the first is needed.  The sum is formed in the same order every time: a thread's values, a wave's lanes, the waves.  The 16-bit copies are stored past the caches
+// (512 x 4096 takes 4.9 us so, 6.3 with ordinary stores; 4095 x 8192 54.7 and 56.8, on buffers in turn).  Memory bounds it: 4095 x 8192 with residual and both copies takes 50 to 55 us,
+// 5.5 to 6.0 TB/s where a copy reaches 6.3; 1 x 4096 takes 2.0, a launch's.
+template <int T, int CH, bool RESIDUAL>
 __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
 {
     __shared__ float part[T / 64];
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
             widen8(r[c], f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = (float)(__bf16)(v[c][i] + f[i]);   // the stream that is kept is the one that is normed
-            if (col < a.K) store8<MANY>(a.residual_out + row * a.K + col, v[c]);
+            if (col < a.K) store8(a.residual_out + row * a.K + col, v[c]);
         }
         float part_sum = 0.0f;
 #pragma unroll
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
             widen8(w[c], f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * f[i];
-            if (a.norm_out) store8<MANY>(a.norm_out + row * a.K + col, v[c]);
+            if (a.norm_out) store8(a.norm_out + row * a.K + col, v[c]);
             quantize8(v[c], a.codes + row * a.K + col, a.scales + row * (a.K / 128) + col / 128, lane);
         }
     }
@@ -191,7 +192,8 @@ struct WeightArgs {
     float* scales;
 };
 
-// A 128 x 128 block to a workgroup: eight rows of 16-byte loads in each thread.
+// A 128 x 128 block to a workgroup, in its threads' registers between its maximum and its codes: sixteen lanes to a row's 128, eight rows to a thread.  Memory bounds it: 57344 x 8192 takes
+// 234 us, 6.0 TB/s (265 with ordinary loads and stores: both ends are read or written once).
 __global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
 {
     __shared__ uint32_t part[4];
@@ -222,13 +224,13 @@ __global__ __launch_bounds__(256) void fp8_quantize_weights_kernel(WeightArgs a)
 // (a launch takes fewer than 2^32 threads: very many rows in several)
 constexpr int64_t kNormRows = 1 << 21;
 
-template <int T, int CH, bool MANY>
+template <int T, int CH>
 hipError_t launch_norm(NormArgs a, hipStream_t st)
 {
     for (int64_t left = a.rows; left > 0; left -= kNormRows) {
         const dim3 grid((unsigned)(left < kNormRows ? left : kNormRows));
-        if (a.residual) hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, true, MANY>), grid, dim3(T), 0, st, a);
-        else hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, false, MANY>), grid, dim3(T), 0, st, a);
+        if (a.residual) hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, true>), grid, dim3(T), 0, st, a);
+        else hipLaunchKernelGGL((fp8_rmsnorm_kernel<T, CH, false>), grid, dim3(T), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         a.x += kNormRows * a.x_stride;
@@ -260,24 +262,18 @@ hipError_t launch_fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const vo
 {
     const NormArgs a{static_cast<const __bf16*>(x), static_cast<const __bf16*>(residual), static_cast<const __bf16*>(weight), static_cast<__bf16*>(residual_out),
                      static_cast<__bf16*>(norm_out), static_cast<uint8_t*>(codes), scales, x_stride, rows, (int)K, eps};
-    // Many rows: sixteen values to a thread.  Few: eight, so that a row takes the shorter.
+    // Eight values to a thread while a row then has 512 threads at most (4095 x 4096: 28.5 us, with sixteen 29.4), or where there is a row or less to a compute unit (256 x 8192:
+    // 4.9 and 5.0, 1 x 8192 3.1 and 3.2); else sixteen (4095 x 8192: 54.7, with eight 55.2; 1024 x 8192 16.3 and 17.0), and more where a row needs them.
     const int64_t n8 = K / 8;
-    if (rows > 2 * compute_units()) {
-        if (n8 <= 128) return launch_norm<64, 2, true>(a, st);
-        if (n8 <= 256) return launch_norm<128, 2, true>(a, st);
-        if (n8 <= 512) return launch_norm<256, 2, true>(a, st);
-        if (n8 <= 1024) return launch_norm<512, 2, true>(a, st);
-        if (n8 <= 2048) return launch_norm<1024, 2, true>(a, st);
-    } else {
-        if (n8 <= 64) return launch_norm<64, 1, false>(a, st);
-        if (n8 <= 128) return launch_norm<128, 1, false>(a, st);
-        if (n8 <= 256) return launch_norm<256, 1, false>(a, st);
-        if (n8 <= 512) return launch_norm<512, 1, false>(a, st);
-        if (n8 <= 1024) return launch_norm<1024, 1, false>(a, st);
-        if (n8 <= 2048) return launch_norm<1024, 2, false>(a, st);
-    }
-    if (n8 <= 4096) return launch_norm<1024, 4, false>(a, st);
-    return launch_norm<1024, 8, false>(a, st);
+    if (n8 <= 64) return launch_norm<64, 1>(a, st);
+    if (n8 <= 128) return launch_norm<128, 1>(a, st);
+    if (n8 <= 256) return launch_norm<256, 1>(a, st);
+    if (n8 <= 512) return launch_norm<512, 1>(a, st);
+    if (n8 <= 1024 && rows <= compute_units()) return launch_norm<1024, 1>(a, st);
+    if (n8 <= 1024) return launch_norm<512, 2>(a, st);
+    if (n8 <= 2048) return launch_norm<1024, 2>(a, st);
+    if (n8 <= 4096) return launch_norm<1024, 4>(a, st);
+    return launch_norm<1024, 8>(a, st);
 }
 
 hipError_t launch_fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes, float* scales, hipStream_t st)

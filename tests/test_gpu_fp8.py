@@ -145,7 +145,7 @@ def test_rmsnorm_of_more_rows_than_a_launch_has(fp4):
     w = torch.randn(K, device="cuda").to(torch.bfloat16)
     norm = torch.empty_like(x)
     got = fp4.fp8_rmsnorm_quantize(x, w, 1e-5, residual=r, norm_out=norm) + (norm,)
-    for part in (slice(0, first), slice(first, rows)):       # (600 rows take the kernel of many rows too: the same bits)
+    for part in (slice(0, first), slice(first, rows)):       # (the same kernel: the same bits)
         n = torch.empty_like(x[part])
         want = fp4.fp8_rmsnorm_quantize(x[part], w, 1e-5, residual=r[part], norm_out=n) + (n,)
         for g, e in zip(got, want):
