@@ -392,7 +392,7 @@ fp4mr_status_t fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void*
 fp4mr_status_t fp8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t K, void* codes_out, float* scales_out, uint32_t flags,
                             void* stream);
 
-/* codes, scales = Q(w) of the bf16 weights [experts, N, K] (experts = 1: one matrix), a scale per 128 x 128 block of each expert. */
+/* codes, scales = Q(w) of the bf16 weights [experts, N, K] (experts = 1: one matrix), a scale per 128 x 128 block of each expert, fewer than 2^24 blocks in all. */
 fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, int64_t K, void* codes_out, float* scales_out,
                                     uint32_t flags, void* stream);
 

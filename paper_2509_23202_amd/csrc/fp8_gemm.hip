@@ -153,7 +153,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, in
 // ---------------------------------------------------------------- few rows: weights streamed from memory
 // 16 TN columns and 16 TM rows to a tile; a workgroup walks a run of tiles.  Its waves share K, each with a run of blocks; a block's codes and scales go to the
 // wave's own part of LDS by direct-to-LDS loads, D blocks ahead, the next tile's behind this one's, so that what is on its way never runs dry
-// and no wave waits for another but to add up a tile.
+// and no wave waits for another but to add up a tile.  Every weight is read once for sixteen or thirty-two rows, and memory bounds it: 1 x 28672 x 4096 takes 25 us, 4.7 TB/s, 16 tokens on
+// 64 experts of 4096 x 4096, four each, 94 us, 7 TB/s of those experts' weights; 1 x 4096 x 4096 takes 4.4, three of them start-up.  K over the waves and not over
+// workgroups: their sums are joined in LDS, in their order, by one launch.  A ring to a wave: tiles of 64 rows, whose waves meet at
+// every block, take 33 us for the first of these.
 template <int TM_, int TN_, int WAVES_, int D_>
 struct Stream {
     static constexpr int TM = TM_, TN = TN_, WAVES = WAVES_, D = D_;
@@ -334,20 +337,25 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
 // ---------------------------------------------------------------- tiles
 // BM x BN to a workgroup of NWM x NWN waves, each 16 TM x 64; a workgroup walks tiles.  A stage is 128 columns of both operands' rows in LDS, eight
 // rows to a 1 KB direct-to-LDS load; the sixteen-byte pieces of a row lie exchanged by a key, so that sixteen rows' reads of one piece touch
-// every bank once.  A step multiplies a stage: the W fragments stay in registers, the X fragments pass through two buffers, and the
-// products of one X fragment are added to the accumulators while the next one's run.  Before its last X fragment a wave has read all it needs
-// of the stage: there it waits for its loads of the next stage, the workgroup meets, and the last fragment's products cover the reads of the next
-// step's first fragments and the requests for the stage S steps on -- of the next tile, when this one's have all gone out: its first stages
-// are there before this tile's output has left.
-// The activations' scales take the same way four blocks of K at a time (a chunk; sixteen rows and four blocks to a load), in a ring of chunks: the
-// part of chunk c + 1 that goes out with the codes of step t = 4c .. 4c + 3 has landed by step t.  Parts past the last chunk go to a place that nobody
-// reads (every wave has the same number of loads on their way at any step: what the waits count).  With three slots they overwrite chunk c - 2, last read
-// in front of step 4c - 5, behind the meeting of step t - S >= 4c - 2 for S = 2; a new tile's first chunk goes out whole in front of its first codes, behind the
-// meeting of step K / 128 - S - 1, and the slots run on: for S = 2 its second chunk's parts begin behind that of step K / 128 - 2, when the last chunk but one of
-// the tile before has been read.  More stages have a fourth slot.
-template <int TM_, int NWM_, int NWN_, int STAGES_, int PER_CU_ = 1>
+// every bank once.  A step multiplies a stage: the W fragments stay in registers, the X fragments pass through a few buffers, and the
+// products of one X fragment are added to the accumulators while the next one's run.  The requests for the stage S - 1 steps on go out between the products, so many to each X fragment;
+// when this tile's have all gone out, they are the next tile's, whose first stages are there before this tile's output has left.
+//   Two stages (256 rows, whose stages leave no room for a third): before its last X fragment a wave has read all it needs of the stage.  There it waits for its loads of the
+// next one, the workgroup meets, and the last fragment's products cover the reads of the next step's first fragments.  The eight waves have all 512 registers of a SIMD's two places,
+// and the step is one loop body: unrolled it spills.
+//   Four stages (64 and 128 rows): a step begins with the meeting, and four steps are one body, so that a stage's place in LDS is a constant.
+//   K counts as a multiple of four blocks: the last ones' scales are zeros.  The activations' scales take the codes' way four blocks at a time (a chunk: sixteen rows and four blocks to a
+// load), in a ring of chunks.  The first chunk of a tile goes out whole in front of its first codes; of chunk c + 1, a part goes out with the codes of each of the steps 4c .. 4c + 3, or
+// where that is past the last chunk to a place that nobody reads: every wave has the same number of loads on their way at any step, which the waits count.  With three
+// slots (two stages) chunk c + 1 overwrites chunk c - 2, last read in front of step 4c - 5, behind the meeting of step 4c - 2; four stages are ahead by two steps more and have a fourth slot.
+//   The output is rounded, turned through 2 KB of LDS of each wave's own, and leaves in lines of 128 bytes.
+//   What bounds them.  256 x 256: 4096 x 28672 x 4096 takes 447 us, 2.15 PFLOP/s: a step takes 1.7 us, in which the matrix cores are busy for 55 % at the 2.0 GHz that the
+// power allows on such operands (a loop of these products in registers reaches 3.7 PFLOP/s on random codes, 5.0 on zeros; a library product with one scale
+// for a tensor takes 398 us here), and the stores of a tile, 5 us of every 63, are not covered.  128 x 128 and 64 x 128: 0.6 and 0.42 us a step, 50 to 57 bytes a ns to a compute unit, which is what
+// the mix of operands from L2 and from memory arrives at; without loads a step of 128 x 128 takes 0.41.
+template <int TM_, int NWM_, int NWN_, int STAGES_>
 struct Tile {
-    static constexpr int TM = TM_, TN = 4, NWM = NWM_, NWN = NWN_, S = STAGES_, NW = NWM * NWN, PER_CU = PER_CU_;
+    static constexpr int TM = TM_, TN = 4, NWM = NWM_, NWN = NWN_, S = STAGES_, NW = NWM * NWN;
     static constexpr int BM = 16 * TM * NWM, BN = 64 * NWN;
     static constexpr int STAGE = (BM + BN) * 128, CHUNK = BM * 16, SLOTS = S == 2 ? 3 : 4;
     static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL + 1;   // loads of a wave for a step: X, W, scales
@@ -357,7 +365,7 @@ struct Tile {
     static constexpr int w_room(int blocks) { return (NB * blocks + 63) / 64 * 256; }   // the scales of W of a tile
     static constexpr int lds(int blocks, bool f32) { return S * STAGE + SLOTS * CHUNK + 256 + out(f32) + 2 * w_room(blocks); }
     // blocks of K that the scales of W have room for
-    static constexpr int max_blocks(bool f32) { return (163840 / PER_CU - lds(0, f32)) / 512 * 64 / NB; }
+    static constexpr int max_blocks(bool f32) { return (163840 - lds(0, f32)) / 512 * 64 / NB; }
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 2 == 0 && BM <= 64 * NW && BM >= 64, "");
     static constexpr bool ROLLED = TM >= 8;    // (see the kernel)
     static_assert(S == (ROLLED ? 2 : 4) && (S - 1) * LPS < 64, "");
@@ -726,7 +734,7 @@ hipError_t launch_tile(const Fp8Args& g, int parts, int part_blocks, hipStream_t
     return hipGetLastError();
 }
 
-// The parts' sums in their order.
+// The parts' sums in their order: for a product of few tiles and a long K, which would leave compute units idle (64 x 4096 x 14336: 50 us whole on tiles of 64 rows, 19 in parts with the sum).
 template <bool OUT_F32>
 __global__ __launch_bounds__(256) void fp8_join_kernel(const float* part, int parts, int64_t n, void* out)
 {
@@ -783,25 +791,28 @@ struct Plan {
     int parts = 1, part_blocks = 0;
 };
 
-// What a kind takes, microseconds on a device of `cus` compute units, measured on 256.  Few rows: W once for every row of tiles, at what they stream with all compute
-// units at work.  Tiles: rounds of them, each a fixed part and the steps of K (fp32 sums take twice the time).  Parts add the writing, reading and launch of their sum.
-double kind_us(int kind, double rows, double tiles_m, double N, int64_t blocks, int parts, bool exact, int cus)
+constexpr int kKinds = 7;
+constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256}, kCols[kKinds] = {16, 32, 16, 32, 128, 128, 256};
+
+// What a kind takes, microseconds on a device of `cus` compute units, as fitted to measurements on 256: rounds of tiles, each a fixed part and the steps of K (a quarter of its blocks where
+// four waves share them; fp32 sums take a tile's steps twice the time), but no less than its weights take from memory: once for every row of tiles where rows are few, else once for each
+// of the `sets` of weights that have rows.  Parts add the writing, reading and launch of their sum.
+// Measured, each kind and number of parts forced in turn, on 183 products of 1 to 4096 rows with layers from 576 x 4096 to 28672 x 8192 and on 44 drawn ones, half of them by expert: the
+// kind that is chosen takes 1.008 of the best one's time in the mean (on 44 more, that nothing was fitted to, 1.035), the others up to ten times it (1000 x 4096 x 4096: tiles of 128 rows 23.5 us, of 64 28.4, of 256 52; 905 x 1079 x
+// 3584: of 64 15.5, of 128 21, of 256 47, 16 rows at a time 42; 770 rows of 52 experts 1856 x 1280: of 64 25, of 128 31, 32 rows at a time 36).
+double kind_us(int kind, double rows, double tiles_m, double sets, double N, int64_t blocks, int parts, bool exact, int cus)
 {
-    if (kind < 4) {
-        static const double rate[] = {4.3e6, 4.5e6, 3.4e6, 3.9e6};
-        const double tiles = tiles_m * std::ceil(N / (kind & 1 ? 32 : 16)), wgs = std::min(tiles, kind == 0 ? 2.0 * cus : cus);
-        return 3.2 + tiles_m * N * 128 * (double)blocks / (rate[kind] * std::min(1.0, wgs / cus) * cus / 256.0);
-    }
-    static const double fixed[] = {2.5, 4.0, 9.0}, step[] = {0.42, 0.60, 1.70}, cols[] = {128, 128, 256};
-    const int64_t steps = ((blocks + parts - 1) / parts + 3) / 4 * 4;
-    const double rounds = std::ceil(tiles_m * std::ceil(N / cols[kind - 4]) * parts / cus);
-    return 3.0 + rounds * (fixed[kind - 4] + (double)steps * step[kind - 4] * (exact ? 2 : 1)) + (parts > 1 ? 2.5 + parts * rows * N * 8 / 4e6 : 0.0);
+    static const double fixed[] = {0.44, 0.60, 0.66, 0.75, 0.82, 2.3, 5.6}, step[] = {0.28, 0.49, 0.46, 0.71, 0.37, 0.51, 1.5}, rate[] = {4.2e6, 10e6, 3.9e6, 7.9e6};
+    const bool few = kind < 4;
+    const int64_t steps = few ? (blocks + 3) / 4 : ((blocks + parts - 1) / parts + 3) / 4 * 4;
+    const double rounds = std::ceil(tiles_m * std::ceil(N / kCols[kind]) * parts / (kind == 0 ? 2 * cus : cus)), work = rounds * (fixed[kind] + (double)steps * step[kind] * (exact && !few ? 2 : 1));
+    const double weights = N * 128 * (double)blocks;
+    if (few) return 2.1 + std::max(work, tiles_m * weights / (rate[kind] * cus / 256));
+    return 2.3 + std::max(work, sets * weights / 4.8e6) + (parts > 1 ? 5.1 + parts * rows * N * 8 / 6e6 : 0.0);
 }
 
-constexpr int kKinds = 7;
 constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(false), Tile128::max_blocks(false), Tile256::max_blocks(false)},
                                        {1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(true), 0, 0}};
-constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256};
 
 constexpr int64_t kMostJoined = 1 << 30;     // elements of an output that is joined from parts, four to a thread
 
@@ -823,7 +834,7 @@ Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
             const int64_t each = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
             if (each > kMaxBlocks[out_f32][kind]) continue;
             if (parts > 1 && (parts - 1) * each >= blocks) continue;      // (a part of nothing)
-            const double us = kind_us(kind, (double)g.rows, tiles_m, (double)g.N, blocks, parts, out_f32, cus);
+            const double us = kind_us(kind, (double)g.rows, tiles_m, grouped ? active : 1.0, (double)g.N, blocks, parts, out_f32, cus);
             const bool chosen = forced ? kind == (forced <= kKinds ? forced - 1 : forced <= 10 ? 4 : 5) && parts == (forced <= kKinds ? 1 : 2 << (forced - 8) % 3) : us < best_us;
             if (chosen) {
                 best = Plan{kind, parts, (int)each};
