@@ -816,7 +816,8 @@ constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile
 
 constexpr int64_t kMostJoined = 1 << 30;     // elements of an output that is joined from parts, four to a thread
 
-// The kind that takes least; in parts only where `room` bytes hold their sums.  Kinds of tiles take K from 512 on, where there is room for the scales of W.
+// The kind that takes least; in parts only where `room` bytes hold their sums and fewer would leave compute units idle, and up to sixteen rows one of the first two: in all of the products
+// above one of those came within 2 % of every other (the whole search takes the host 0.5 us, this one 0.2 to 0.4).  Kinds of tiles take K from 512 on, where there is room for the scales of W.
 Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
 {
     const int64_t blocks = g.K >> 7;
@@ -825,12 +826,13 @@ Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
     best.part_blocks = (int)blocks;
     double best_us = 1e30;
     for (int kind = 0; kind < kKinds; ++kind) {
-        if (kind >= 4 && blocks < 4) break;
+        if ((kind >= 4 && blocks < 4) || (kind >= 2 && g.rows <= 16 && !forced)) break;
         // rows of tiles; by expert: as if the rows were spread evenly over the experts, half a tile more to each than they fill
         const double active = (double)std::min<int64_t>(g.experts, g.rows);
         const double tiles_m = grouped ? active * std::max(1.0, (double)g.rows / active / kRows[kind] + 0.4) : (double)((g.rows + kRows[kind] - 1) / kRows[kind]);
         for (int parts = 1; parts <= 16; ++parts) {
             if (parts > 1 && (grouped || kind < 4 || kind > 5 || g.rows * g.N > kMostJoined || (size_t)parts * g.rows * g.N * 4 > room)) break;
+            if (parts > 1 && !forced && (parts - 1) * tiles_m * std::ceil((double)g.N / kCols[kind]) >= cus) break;
             const int64_t each = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
             if (each > kMaxBlocks[out_f32][kind]) continue;
             if (parts > 1 && (parts - 1) * each >= blocks) continue;      // (a part of nothing)
