@@ -724,6 +724,7 @@ __global__ __launch_bounds__(C::NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 template <bool GROUPED, bool EXACT, bool OUT_F32, bool SPLIT, typename C>
 hipError_t launch_tile(const Fp8Args& g, int parts, int part_blocks, hipStream_t st)
 {
+    if (part_blocks > C::max_blocks(OUT_F32)) return hipErrorInvalidValue;      // (a plan keeps to it)
     static LdsAttrOnce attr;
     const hipError_t e = attr.ensure(reinterpret_cast<const void*>(fp8_tile_kernel<GROUPED, EXACT, OUT_F32, SPLIT, C>), 163840);
     if (e != hipSuccess) return e;
@@ -813,6 +814,8 @@ double kind_us(int kind, double rows, double tiles_m, double sets, double N, int
 
 constexpr int kMaxBlocks[2][kKinds] = {{1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(false), Tile128::max_blocks(false), Tile256::max_blocks(false)},
                                        {1 << 15, 1 << 15, 1 << 15, 1 << 15, Tile64::max_blocks(true), 0, 0}};
+// in parts of K: blocks of a part, whose sums leave as fp32 whatever the output is
+constexpr int kMaxPartBlocks[2][kKinds] = {{0, 0, 0, 0, Tile64::max_blocks(true), Tile128::max_blocks(true), 0}, {0, 0, 0, 0, Tile64::max_blocks(true), 0, 0}};
 
 constexpr int64_t kMostJoined = 1 << 30;     // elements of an output that is joined from parts, four to a thread
 
@@ -834,7 +837,7 @@ Plan plan_fp8(const Fp8Args& g, bool grouped, bool out_f32, size_t room)
             if (parts > 1 && (grouped || kind < 4 || kind > 5 || g.rows * g.N > kMostJoined || (size_t)parts * g.rows * g.N * 4 > room)) break;
             if (parts > 1 && !forced && (parts - 1) * tiles_m * std::ceil((double)g.N / kCols[kind]) >= cus) break;
             const int64_t each = parts == 1 ? blocks : ((blocks + parts - 1) / parts + 3) / 4 * 4;
-            if (each > kMaxBlocks[out_f32][kind]) continue;
+            if (each > (parts > 1 ? kMaxPartBlocks : kMaxBlocks)[out_f32][kind]) continue;
             if (parts > 1 && (parts - 1) * each >= blocks) continue;      // (a part of nothing)
             const double us = kind_us(kind, (double)g.rows, tiles_m, grouped ? active : 1.0, (double)g.N, blocks, parts, out_f32, cus);
             const bool chosen = forced ? kind == (forced <= kKinds ? forced - 1 : forced <= 10 ? 4 : 5) && parts == (forced <= kKinds ? 1 : 2 << (forced - 8) % 3) : us < best_us;

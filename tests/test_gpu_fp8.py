@@ -482,3 +482,55 @@ def test_refusals_of_the_binding(fp4):
                  lambda: fp4.fp8_rmsnorm_quantize(x, x[0].contiguous(), residual_out=torch.empty_like(x))):
         with pytest.raises((fp4.Fp4mrError, AssertionError)):
             call()
+
+
+def ternary(M, N, K, seed):
+    """Operands of -1, 0 and 1 with scales of 1 and 2, whose products' sums are whole numbers below 2^24 in any order (K < 2^22), and that product."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    out = []
+    for rows, per in ((M, 1), (N, 128)):
+        v = torch.randint(-1, 2, (rows, K), generator=g, device="cuda", dtype=torch.int8)
+        s = 1.0 + torch.randint(0, 2, (-(-rows // per), K // 128), generator=g, device="cuda").float()
+        out += [v.to(torch.float8_e4m3fn), s, v.double() * s.repeat_interleave(per, 0)[:rows].repeat_interleave(128, 1).double()]
+    a, sa, A, w, sw, W = out
+    return (a, sa, w, sw), A @ W.t()
+
+
+@pytest.mark.parametrize("kernel,parts,blocks,f32", [(7, 1, 224, False), (7, 1, 225, False), (6, 1, 1984, False), (6, 1, 1985, False), (5, 1, 6592, False), (5, 1, 6593, False), (5, 1, 5568, True),
+                                                     (5, 1, 5569, True), (11, 2, 960, False), (11, 2, 964, False), (13, 8, 960, False), (13, 8, 964, False), (8, 2, 5568, False), (8, 2, 5572, False),
+                                                     (8, 2, 5568, True), (8, 2, 5572, True)])
+def test_products_at_the_room_for_scales(fp4, forced, kernel, parts, blocks, f32):
+    """The longest K, and the longest part of K, whose weights' scales fit beside a tile's stages, and the next one, which runs on another kernel: exact."""
+    M, N, K = 17, 136, 128 * (blocks if parts == 1 else parts * blocks - 3)
+    say(f"kernel {kernel} K={K} in {parts} parts of {blocks} blocks, f32={f32}")
+    forced(kernel)
+    ops, y = ternary(M, N, K, blocks)
+    room = torch.full((16 * M * N * 4,), 0xff, dtype=torch.uint8, device="cuda") if parts > 1 else None
+    out = fp4.fp8_gemm(*ops, flags=fp4.OUT_F32 if f32 else 0, workspace=room)
+    assert torch.equal(out, y.to(out.dtype))
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_a_k_that_no_tile_takes_without_a_workspace(fp4, f32):
+    M, N, K = 40, 72, 128 * 6600
+    ops, y = ternary(M, N, K, 1)
+    out = torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    status = fp4.lib.fp8_gemm(*(t.data_ptr() for t in ops), M, N, K, out.data_ptr(), None, 0, fp4.OUT_F32 if f32 else 0, torch.cuda.current_stream().cuda_stream)
+    assert status == 0 and torch.equal(out, y.to(out.dtype))
+
+
+def test_a_long_k_in_the_parts_that_the_library_asks_for(fp4):
+    """1024 x 2048 x 262144 with the workspace of fp8_workspace_bytes: parts of 1024 blocks would leave the scales no room on tiles of 128 rows."""
+    M, N, K = 1024, 2048, 262144
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    rnd = lambda rows: torch.randint(-1, 2, (rows, K), generator=g, device="cuda", dtype=torch.int8).to(torch.float8_e4m3fn)
+    a, w = rnd(M), rnd(N)
+    sa, sw = torch.ones(M, K // 128, device="cuda"), torch.ones(N // 128, K // 128, device="cuda")
+    sa[:, 1::3] = 2.0
+    out = fp4.fp8_gemm(a, sa, w, sw)
+    rows, cols = torch.arange(3, M, 31, device="cuda"), torch.arange(5, N, 61, device="cuda")
+    u8 = lambda t, i: t.view(torch.uint8)[i].view(torch.float8_e4m3fn).double()
+    y = (u8(a, rows) * sa[rows].repeat_interleave(128, 1).double()) @ u8(w, cols).t()
+    assert torch.equal(out[rows][:, cols], y.to(torch.bfloat16))
