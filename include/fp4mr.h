@@ -415,7 +415,8 @@ size_t fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, uint32_t flags);
  *   offsets      device int32 [experts + 1], not decreasing, 0 .. rows (a number outside that range counts as the nearest within it); an
  *                expert may have no rows.  Rows of out that no expert has are not written.
  *   index        device int32 [rows], the row of A for each row of out (so that a token's row is read by each of its experts from one
- *                place), or NULL: row t of A for row t of out, a_rows == rows.  A negative index, or one of a_rows or more, stands for a row of zeros.
+ *                place), or NULL: row t of A for row t of out, a_rows == rows.  A negative index, or one of a_rows or more, stands for a row of zeros
+ *                (codes and scales): its outputs are 0, but NaN where the weights that they read hold a NaN or a scale that is not finite.
  * offsets and index need 4-byte alignment only.  rows and a_rows <= 2^24, experts <= 65536, experts * N <= 2^31; with an index, a_rows * K <=
  * 0xf0000000.  Offsets that decrease are not an error that the call can see: which products the rows then hold is not defined.
  */

@@ -167,6 +167,9 @@ struct Stream {
     static_assert(TM <= 3 && lds() <= 163840 && D * LOADS < 64, "");
 };
 
+// The scale, whichever block it is of, of a row that an index outside A stands for.
+__device__ const float kZeroRowScale = 0.0f;
+
 template <bool GROUPED, bool OUT_F32, typename C>
 __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, int tiles_m, int tiles_n)
 {
@@ -192,6 +195,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
     __amdgpu_buffer_rsrc_t rw, rx;
     uint32_t xo[TM][2];
     const float* scale = nullptr;
+    int scale_on = -1;         // 0: the same for every block
     Rows r{0, 0, 0};
     int n0 = 0, at_m = -1;
     auto locate = [&](int tile) {
@@ -215,8 +219,11 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
                     xo[t][h] = (row < x_rows ? (uint32_t)row * (uint32_t)K : kOutside) + (piece ^ (4 * h)) * 16;
                 }
             int64_t row = x_row(min(lane, 16 * TM - 1));
-            if (row == x_rows) row = 0;               // (any: its codes are zeros, and the output's row is not stored or is set to zero)
+            const bool none = row == x_rows;
+            if (none) row = 0;                        // (any: its codes are zeros, and the output's row is not stored)
             scale = g.a_scales + (x0 + row) * KB;
+            if (gather && none) scale = &kZeroRowScale;
+            if constexpr (GROUPED) scale_on = gather && none && lane != 63 ? 0 : -1;
         }
         rw = make_rsrc(g.w + ((int64_t)r.expert * g.N + n0) * K, (int64_t)min((int)g.N - n0, 16 * TN) * K);
         if (lane == 63) scale = g.w_scales + ((int64_t)r.expert * blocks_n + (n0 >> 7)) * KB;
@@ -234,7 +241,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
             load_lds16(rx, smem, to + (TN + t) * 2048, xo[t][0], kb * 128);
             load_lds16(rx, smem, to + (TN + t) * 2048 + 1024, xo[t][1], kb * 128);
         }
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uintptr_t>(scale + kb)),
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) void*>(reinterpret_cast<uintptr_t>(scale + (GROUPED ? kb & scale_on : kb))),
                                          (lds_void*)((lds_char*)smem + to + (TN + TM) * 2048), 4, 0, 0);
         load_slot = load_slot == D - 1 ? 0 : load_slot + 1;
         if (++load_kb == each) {
@@ -315,7 +322,6 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
             for (int v = 1; v < WAVES; ++v) sum += part[(v * TM * TN + q) * 64 + lane];
             const int m = mine.begin + 16 * (q / TN) + l16, n = col0 + 16 * (q % TN) + (lane >> 4) * 4;
             if (m >= mine.end) continue;
-            if (gather && (uint32_t)g.index[m] >= (uint64_t)g.a_rows) sum = v4f{0.f, 0.f, 0.f, 0.f};
             const int64_t o = (int64_t)m * g.N + n;
             const int have = (int)g.N - n;
             if constexpr (OUT_F32) {

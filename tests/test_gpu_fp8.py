@@ -534,3 +534,36 @@ def test_a_long_k_in_the_parts_that_the_library_asks_for(fp4):
     u8 = lambda t, i: t.view(torch.uint8)[i].view(torch.float8_e4m3fn).double()
     y = (u8(a, rows) * sa[rows].repeat_interleave(128, 1).double()) @ u8(w, cols).t()
     assert torch.equal(out[rows][:, cols], y.to(torch.bfloat16))
+
+
+def experts_that_are_not_finite(E, N, K):
+    """Weights of E >= 2 experts: of the first a code in row 5 is NaN, of the second the scale of its rows 128 to 255 and one block of K is infinite."""
+    w, sw = R.operand(E * -(-N // 128) * 128, K, 2, 128, 0.01)
+    w, sw = w.view(torch.uint8).view(E, -1, K)[:, :N].contiguous(), sw.view(E, -1, K // 128).clone()
+    w[0, 5, 200] = 0x7f
+    sw[1, 1, 3] = float("inf")
+    return w.view(torch.float8_e4m3fn), sw
+
+
+@pytest.mark.parametrize("kernel,f32", [(k, False) for k in KERNELS] + [(k, True) for k in KERNELS[:5]])     # (tiles of 128 and 256 rows have no fp32 output)
+def test_an_index_outside_is_a_row_of_zeros_on_every_kernel(fp4, forced, kernel, f32):
+    """Zero codes with a scale of zero: 0, and NaN beside weights that hold a NaN or an infinite scale, whatever the rows of A hold."""
+    forced(kernel)
+    K, N, counts = 640, 300, [90, 150]
+    T = sum(counts)
+    a, sa = R.operand(10, K, 1)
+    sa[0] = float("nan")
+    a.view(torch.uint8)[9] = 0x7f
+    w, sw = experts_that_are_not_finite(2, N, K)
+    index = torch.full((T,), 4, dtype=torch.int32)
+    outside = [0, 1, 17, 63, 64, 89, 90, 91, 130, 200, 239]
+    index[outside] = torch.tensor([-1, 10, 2 ** 31 - 1, -2 ** 31, 11, -7, 10, -1, 4096, -1, 10], dtype=torch.int32)
+    out = fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor([0, 90, T], dtype=torch.int32, device="cuda"), rows=index.cuda(), flags=fp4.OUT_F32 if f32 else 0).float().cpu()
+    row = torch.zeros(2, N)
+    row[0, 5] = float("nan")
+    row[1, 128:256] = float("nan")
+    for t in outside:
+        assert torch.equal(out[t].nan_to_num(7.0), row[int(t >= 90)].nan_to_num(7.0)), t
+    inside = [t for t in range(T) if t not in outside]
+    for t in inside:
+        assert torch.equal(torch.isfinite(out[t]), torch.isfinite(row[int(t >= 90)]))
