@@ -456,6 +456,7 @@ def fp8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None, 
     need = fp8_workspace_bytes(M, N, K, flags)
     if need and workspace is None:
         workspace = (a_codes.new_empty if type(a_codes) is _Tensor else _plain_empty(a_codes))(need, dtype=torch.uint8)
+    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous())
     wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.fp8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, out.data_ptr(), _ptr(workspace), wsz, flags, _stream()))
     return out

@@ -84,3 +84,26 @@ def test_workspace(b):
     assert b.fp8_workspace_bytes(4096, 4096, 4096) == 0 and b.fp8_workspace_bytes(1, 4096, 4096) == 0 and b.fp8_workspace_bytes(0, 4096, 4096) == 0
     assert b.fp8_workspace_bytes(200, 4096, 100) == 0
     assert b.lib.fp4_set_option(b.OPT_FP8_VARIANT, 14) == 4 and b.lib.fp4_set_option(b.OPT_FP8_VARIANT, -1) == 4
+
+
+def test_a_workspace_is_device_memory_of_its_own_size(b, monkeypatch):
+    """A workspace in host memory, or of fewer bytes than its shape counts, is refused in front of the library, which would have the device write to it."""
+    import torch
+
+    class OnDevice(torch.Tensor):       # (host memory that says it is the device's: nothing is launched)
+        is_cuda = True
+
+    calls = []
+    monkeypatch.setattr(b, "_stream", lambda: 0)
+    monkeypatch.setattr(b.lib, "fp8_gemm", lambda *a: calls.append(a) or 0)
+    M, N, K = 64, 256, 4096
+    on = lambda *shape, dtype: torch.empty(shape, dtype=dtype).as_subclass(OnDevice)
+    a, w = on(M, K, dtype=torch.float8_e4m3fn), on(N, K, dtype=torch.float8_e4m3fn)
+    sa, sw, out = (on(*s, dtype=torch.float32) for s in ((M, K // 128), (N // 128, K // 128), (M, N)))
+    room = lambda n: torch.empty(n, dtype=torch.uint8)
+    for bad in (room(1 << 20), room(1).expand(1 << 20).as_subclass(OnDevice), room(1 << 20).as_subclass(OnDevice)[::2]):
+        with pytest.raises(AssertionError):
+            b.fp8_gemm(a, sa, w, sw, flags=b.OUT_F32, out=out, workspace=bad)
+    assert not calls
+    b.fp8_gemm(a, sa, w, sw, flags=b.OUT_F32, out=out, workspace=room(1 << 20).as_subclass(OnDevice))
+    assert len(calls) == 1 and calls[0][9] == 1 << 20
