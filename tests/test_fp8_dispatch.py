@@ -120,3 +120,13 @@ def test_parts_take_k_up_to_the_room_for_scales(host, kernel, parts, tile, flags
     at, over = held(at), held(over)
     assert tile in at[0]["kernel"] and "fp8_join" in at[1]["kernel"] and at[1]["parts"] == parts
     assert len(over) == 1 and "fp8_stream" in over[0]["kernel"]
+
+
+@pytest.mark.parametrize("flags", [BF16, F32])
+def test_forced_parts_are_the_ones_that_tests_on_the_device_name(host, flags):
+    for kernel in range(8, 14):
+        run = held(host(["kernel", kernel], ["gemm", 70, 300, 3840, flags, 8 * 70 * 300 * 4])[1])
+        if flags == F32 and kernel > 10:       # (tiles of 128 rows have no fp32 output)
+            assert len(run) == 1 and "fp8_stream" in run[0]["kernel"]
+        else:
+            assert (TILE64 if kernel <= 10 else TILE128) in run[0]["kernel"] and run[1]["parts"] == 2 << (kernel - 8) % 3

@@ -567,3 +567,80 @@ def test_an_index_outside_is_a_row_of_zeros_on_every_kernel(fp4, forced, kernel,
     inside = [t for t in range(T) if t not in outside]
     for t in inside:
         assert torch.equal(torch.isfinite(out[t]), torch.isfinite(row[int(t >= 90)]))
+
+
+@pytest.mark.parametrize("kernel", KERNELS + list(range(8, 14)))
+@pytest.mark.parametrize("f32", [False, True])
+def test_numbers_that_are_not_finite_stay_in_their_rows_and_columns(fp4, forced, kernel, f32):
+    """On every kernel and in every number of parts, of a K that is not a multiple of four blocks, the last of which are multiplied again with scales of zero: a code that is NaN, a scale that
+    is NaN or infinite, of either operand, in the first, the last and other blocks.  (Those kernels that have no fp32 output leave it to another.)"""
+    forced(kernel)
+    M, N, K = 70, 300, 128 * 30
+    (a, sa), (w, sw) = R.operand(M, K, 1), R.operand(N, K, 2, 128, 0.01)
+    A, W = R.values(a, sa), R.values(w, sw, 128)
+    a.view(torch.uint8)[3, K - 100] = 0x7f
+    a.view(torch.uint8)[64, 0] = 0xff
+    sa[40, 2], sa[41, 29] = float("inf"), float("nan")
+    w.view(torch.uint8)[7, 5] = 0xff
+    w.view(torch.uint8)[100, K - 1] = 0x7f
+    sw[1, 28], sw[2, 0] = float("inf"), float("nan")
+    out = fp4.fp8_gemm(a, sa, w, sw, flags=fp4.OUT_F32 if f32 else 0, workspace=torch.full((8 * M * N * 4,), 0xff, dtype=torch.uint8, device="cuda"))
+    rows, cols = [m for m in range(M) if m not in (3, 40, 41, 64)], [n for n in range(128) if n not in (7, 100)]
+    good = torch.zeros(M, N, dtype=torch.bool)
+    good[np.ix_(rows, cols)] = True
+    assert torch.equal(torch.isfinite(out).cpu(), good)
+    R.check_product(out[rows][:, cols], A[rows], W[cols], K)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_numbers_that_are_not_finite_stay_with_their_expert(fp4, forced, kernel):
+    forced(kernel)
+    K, N, counts = 128 * 6, 300, [90, 150, 40]
+    T, begin = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    a, sa = R.operand(T, K, 3)
+    w, sw = experts_that_are_not_finite(3, N, K)
+    A = R.values(a, sa)
+    sa[89, 5] = float("inf")            # (the last row of the first expert)
+    a.view(torch.uint8)[240, 0] = 0x7f  # (the first one of the third)
+    out = fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor(begin, dtype=torch.int32, device="cuda"))
+    good = torch.ones(T, N, dtype=torch.bool)
+    good[[89, 240]] = False
+    good[:90, 5] = False
+    good[90:240, 128:256] = False
+    assert torch.equal(torch.isfinite(out).cpu(), good)
+    for e in range(3):
+        rows = [t for t in range(begin[e], begin[e + 1]) if t not in (89, 240)]
+        cols = [n for n in range(N) if not (e == 0 and n == 5 or e == 1 and 128 <= n < 256)]
+        R.check_product(out[rows][:, cols], A[rows], R.values(w[e], torch.nan_to_num(sw[e], posinf=0.0), 128)[cols], K)
+
+
+def test_a_workgroup_walks_several_tiles_of_an_fp32_output(fp4, forced):
+    """More tiles of 64 x 128 than compute units, of whole and partial rows and columns, seven blocks of K; and as many by expert."""
+    forced(5)
+    M, N, K = 4200, 4440, 896
+    (a, sa), (w, sw) = R.operand(M, K, 1), R.operand(N, K, 2, 128, 0.01)
+    out = fp4.fp8_gemm(a, sa, w, sw, flags=fp4.OUT_F32)
+    rows = np.r_[0:70, 250:260, 2040:2100, 4090:4200]
+    R.check_product(out[rows], R.values(a, sa)[rows], R.values(w, sw, 128), K)
+    cols = np.r_[0:20, 120:132, 250:260, 4090:4110, 4430:4440]
+    R.check_product(out[:, cols].contiguous(), R.values(a, sa), R.values(w, sw, 128)[cols], K)
+    for gather in (None, 333):
+        grouped(fp4, [700, 0, 3, 129, 0, 1100, 64, 257, 1, 400], 1100, 640, 5, gather, f32=True)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("offsets,expert,first,end", [([30, 10, 40, 5], 1, 10, 40), ([0, 50, 50, 20], 0, 0, 50), ([0, 0, 0, 0], 0, 0, 0)])
+def test_rows_of_one_expert_where_offsets_decrease(fp4, forced, kernel, offsets, expert, first, end):
+    """An expert whose offsets decrease has no rows; with the others' apart and no more tiles than the rows have, theirs are their products and the rest stays as it was."""
+    forced(kernel)
+    K, N, T = 640, 200, 50
+    a, sa = R.operand(T, K, 5)
+    w, sw = R.operand(3 * 256, K, 2, 128, 0.01)
+    w, sw = w.view(torch.uint8).view(3, 256, K)[:, :N].contiguous().view(torch.float8_e4m3fn), sw.view(3, 2, K // 128)
+    room = torch.full((T * N * 2 + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+    out = room[32768: -32768].view(torch.bfloat16).view(T, N)
+    fp4.fp8_grouped_gemm(a, sa, w, sw, torch.tensor(offsets, dtype=torch.int32, device="cuda"), out=out)
+    if end > first:
+        R.check_product(out[first:end], R.values(a, sa)[first:end], R.values(w[expert], sw[expert], 128), K)
+        out[first:end].view(torch.uint8).fill_(0x5a)
+    assert (room == 0x5a).all()
