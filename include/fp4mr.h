@@ -369,7 +369,7 @@ fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* st
  *   scale = max(amax, 2^-100) / 448 ,  code = the E4M3 value nearest to  v * (448 / max(amax, 2^-100)) , ties to even ,
  * with amax the block's largest |v| and every operation in binary32.  A block that holds a NaN or an infinity has a scale that is
  * not finite, and every output of a product that reads it is NaN or infinite.
- * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24, in products K <= 2^22 and M N <= 2^38.  No rows (M, or rows, of 0) is not an
+ * K is a multiple of 128 in all calls (FP4MR_ERR_SHAPE), M and N are any sizes; M, N, K <= 2^24, in products K <= 2^22 and M N <= 2^38; N and K are at least 1 and 128.  No rows (M, or rows, of 0) is not an
  * error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.  Scales, and the outputs of products, need the alignment of
  * their elements only (an expert's part of them begins anywhere).
  *
@@ -379,7 +379,8 @@ fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* st
  *                where x_stride == K
  *   weight       bf16 [K];  K <= 65536
  *   norm_out     bf16 [M,K] or NULL: receives v rounded to bf16 (what a router reads)
- * Outputs must not overlap inputs or each other other than as said.  eps >= 0, else FP4MR_ERR_SHAPE.
+ * Outputs must not overlap inputs or each other other than as said.  eps >= 0, else FP4MR_ERR_SHAPE.  A row's squares are added in an order that is
+ * the same every time, but for 4096 < K <= 8192 another one in calls of more rows than there are compute units: last bits of v may then differ.
  */
 fp4mr_status_t fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t M, int64_t K,
                                     float eps, void* codes_out, float* scales_out, void* residual_out, void* norm_out,
@@ -388,6 +389,8 @@ fp4mr_status_t fp8_rmsnorm_quantize(const void* x, int64_t x_stride, const void*
 /*
  * codes, scales = Q(x) of bf16 activations, or with FP4MR_SILU_MUL of  silu(gate) * up , where a row of x is [gate | up], 2K elements.
  * Rows are x_stride elements apart (at least what a row holds, a multiple of 8).  No workspace.
+ * silu(g) = g / (1 + e^-g) in binary32: 0 where e^-g is beyond it (g < -88.7), and from g < -87.3 on, where its reciprocal is subnormal, 0 or near.  A gate of
+ * minus infinity gives NaN, as the quotient does.
  */
 fp4mr_status_t fp8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t K, void* codes_out, float* scales_out, uint32_t flags,
                             void* stream);
@@ -400,7 +403,8 @@ fp4mr_status_t fp8_quantize_weights(const void* w, int64_t experts, int64_t N, i
  * out[M,N] = A W^T  from 8-bit operands: every 128 columns' products are summed by the matrix instruction and added in fp32 with their two
  * scales.  out is bf16, or fp32 with FP4MR_OUT_F32.  For a bf16 output the 8-bit matrix instruction sums eight products at a time and drops what
  * lies below 2^-13 of the largest of them: an output is within (2^-10 + K 2^-31 + 2^-16) sum |a w| of the exact product before its rounding.  For an fp32
- * output the codes are multiplied as fp16 with fp32 sums, at less than half the rate: within (K / 128 + 129) 2^-24 sum |a w|.
+ * output the codes are multiplied as fp16 with fp32 sums: within (K / 128 + 129) 2^-24 sum |a w|, in the same time up to sixteen rows and two to three times as long for thousands.
+ * The two scales of a block are multiplied in binary32 first: beyond its range what a block adds is not finite (NaN where its products add up to zero), below 2^-126 it loses bits.
  *   workspace    optional: with fp8_workspace_bytes(M, N, K, flags) bytes (0 where that is of no use) a product of few tiles and a long K is split
  *                along K over otherwise idle compute units, and its parts' fp32 sums, kept there, are added in a fixed order.  With less, or
  *                NULL, it runs in fewer parts, or in one.  Results of different plans differ in the order of their sums.

@@ -6,7 +6,8 @@
 // fp32 accumulator.  The instruction adds eight products at a time in fewer bits than fp32 has: what lies below 2^-13 of the power of two of
 // the largest of the eight is dropped (measured; every 8-bit MFMA does), 1.4e-5 of a sum of normal values, where a bf16 output is rounded to
 // 2^-9.  Products with an fp32 output are for those who go on with the sums: they multiply the codes as fp16, which holds them, on the fp16
-// MFMA, whose sums are fp32 (at less than half the rate).  The W codes are the MFMA's A operand and the activations its B operand: a lane then has four consecutive n of one
+// MFMA, whose sums are fp32 (4096 x 4096 x 4096: 175 us, 0.79 PFLOP/s, where bf16 takes 63: a step of the 64-row tile, the only one with such sums, takes 0.62 us for 0.32, and the larger tiles do
+// more to a step; few rows take the same time either way).  The W codes are the MFMA's A operand and the activations its B operand: a lane then has four consecutive n of one
 // m, and the one activation scale.  Both operands are row-major, 128 bytes of a row to a step: lane l reads row l % 16, and from the row's
 // eight pieces of 16 bytes the pieces l / 16 and l / 16 + 4 (the product does not care which of the 128 k is which, as long as both
 // operands agree).
@@ -154,7 +155,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, in
 // 16 TN columns and 16 TM rows to a tile; a workgroup walks a run of tiles.  Its waves share K, each with a run of blocks; a block's codes and scales go to the
 // wave's own part of LDS by direct-to-LDS loads, D blocks ahead, the next tile's behind this one's, so that what is on its way never runs dry
 // and no wave waits for another but to add up a tile.  Every weight is read once for sixteen or thirty-two rows, and memory bounds it: 1 x 28672 x 4096 takes 25 us, 4.7 TB/s, 16 tokens on
-// 64 experts of 4096 x 4096, four each, 94 us, 7 TB/s of those experts' weights; 1 x 4096 x 4096 takes 4.4, three of them start-up.  K over the waves and not over
+// 64 experts of 4096 x 4096, four each, 93 us, 7 TB/s of those experts' weights; 1 x 4096 x 4096 takes 4.4 to 5.6 by card, three of them start-up.  K over the waves and not over
 // workgroups: their sums are joined in LDS, in their order, by one launch.  A ring to a wave: tiles of 64 rows, whose waves meet at
 // every block, take 33 us for the first of these.
 template <int TM_, int TN_, int WAVES_, int D_>
@@ -355,9 +356,9 @@ __global__ __launch_bounds__(C::WAVES * 64) void fp8_stream_kernel(Fp8Args g, in
 // where that is past the last chunk to a place that nobody reads: every wave has the same number of loads on their way at any step, which the waits count.  With three
 // slots (two stages) chunk c + 1 overwrites chunk c - 2, last read in front of step 4c - 5, behind the meeting of step 4c - 2; four stages are ahead by two steps more and have a fourth slot.
 //   The output is rounded, turned through 2 KB of LDS of each wave's own, and leaves in lines of 128 bytes.
-//   What bounds them.  256 x 256: 4096 x 28672 x 4096 takes 447 us, 2.15 PFLOP/s: a step takes 1.7 us, in which the matrix cores are busy for 55 % at the 2.0 GHz that the
+//   What bounds them.  256 x 256: 4096 x 28672 x 4096 takes 443 to 460 us, 2.1 PFLOP/s: a step takes 1.75 to 1.85 us, in which the matrix cores are busy for 55 % at the 2.0 GHz that the
 // power allows on such operands (a loop of these products in registers reaches 3.7 PFLOP/s on random codes, 5.0 on zeros; a library product with one scale
-// for a tensor takes 398 us here), and the stores of a tile, 5 us of every 63, are not covered.  128 x 128 and 64 x 128: 0.6 and 0.42 us a step, 50 to 57 bytes a ns to a compute unit, which is what
+// for a tensor takes 398 us here), and the stores of a tile, 5 us of every 63, are not covered.  128 x 128 and 64 x 128: 0.50 to 0.57 and 0.32 to 0.42 us a step, 57 to 77 bytes a ns to a compute unit, which is what
 // the mix of operands from L2 and from memory arrives at; without loads a step of 128 x 128 takes 0.41.
 template <int TM_, int NWM_, int NWN_, int STAGES_>
 struct Tile {
@@ -804,8 +805,11 @@ constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 256}, kCols[kKinds] = {1
 // What a kind takes, microseconds on a device of `cus` compute units, as fitted to measurements on 256: rounds of tiles, each a fixed part and the steps of K (a quarter of its blocks where
 // four waves share them; fp32 sums take a tile's steps twice the time), but no less than its weights take from memory: once for every row of tiles where rows are few, else once for each
 // of the `sets` of weights that have rows.  Parts add the writing, reading and launch of their sum.
+// The constants are a fit to all of those, not a kernel's own figures: large products run their 256-row tiles at the power limit, 1.75 to 1.85 us a step.
 // Measured, each kind and number of parts forced in turn, on 183 products of 1 to 4096 rows with layers from 576 x 4096 to 28672 x 8192 and on 44 drawn ones, half of them by expert: the
-// kind that is chosen takes 1.008 of the best one's time in the mean (on 44 more, that nothing was fitted to, 1.035), the others up to ten times it (1000 x 4096 x 4096: tiles of 128 rows 23.5 us, of 64 28.4, of 256 52; 905 x 1079 x
+// kind that is chosen takes 1.00 to 1.01 of the best one's time in the mean (on 44 more, that nothing was fitted to, 1.02 to 1.035), at worst 1.26 (256 x 1079 x 3584: 14.3 us on whole tiles, 11.3 in
+// parts; 128 x 4096 x 4096: 12.8, 10.7) and by expert 1.37 to 1.46 (6240 rows of 5 experts 544 x 1664: 26 us on tiles of 128 rows, whose 254 in the mean are
+// priced as one round where those experts' numbers of rows make two, 18 on tiles of 64); the others up to ten times it (1000 x 4096 x 4096: tiles of 128 rows 23.5 us, of 64 28.4, of 256 52; 905 x 1079 x
 // 3584: of 64 15.5, of 128 21, of 256 47, 16 rows at a time 42; 770 rows of 52 experts 1856 x 1280: of 64 25, of 128 31, 32 rows at a time 36).
 double kind_us(int kind, double rows, double tiles_m, double sets, double N, int64_t blocks, int parts, bool exact, int cus)
 {

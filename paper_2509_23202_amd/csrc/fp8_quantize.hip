@@ -91,7 +91,7 @@ struct QuantArgs {
 };
 
 // Sixteen lanes to a block of 128, in the order of the outputs: 16-byte loads, a maximum in four lane exchanges, whole lines of codes.  Memory bounds it: gated 4096 x 14336 takes 47 us,
-// 6.3 TB/s, what a copy reaches; 33 x 14336 takes 2.8, a launch's.  (Loads past the caches: an input is read once.)
+// 6.3 TB/s, what a copy reaches; 33 x 14336 takes 2.5 to 2.9, a launch's, and 4096 x 8192 as it is 21, 4.8 TB/s.  (Loads past the caches: an input is read once.)
 template <bool SILU>
 __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantArgs a)
 {
@@ -127,7 +127,7 @@ struct NormArgs {
 // A row to T threads, CH times eight values in each one's registers from the sum of squares to the codes, so that a row is read once; all of a thread's loads are on
 // their way before the first is needed.  The sum is formed in the same order every time: a thread's values, a wave's lanes, the waves.  The 16-bit copies are stored past the caches
 // (512 x 4096 takes 4.9 us so, 6.3 with ordinary stores; 4095 x 8192 54.7 and 56.8, on buffers in turn).  Memory bounds it: 4095 x 8192 with residual and both copies takes 50 to 55 us,
-// 5.5 to 6.0 TB/s where a copy reaches 6.3; 1 x 4096 takes 2.0, a launch's.
+// 5.5 to 6.0 TB/s where a copy reaches 6.3; 1 x 4096 takes 2.2 to 2.7, a launch's.
 template <int T, int CH, bool RESIDUAL>
 __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
 {

@@ -644,3 +644,17 @@ def test_rows_of_one_expert_where_offsets_decrease(fp4, forced, kernel, offsets,
         R.check_product(out[first:end], R.values(a, sa)[first:end], R.values(w[expert], sw[expert], 128), K)
         out[first:end].view(torch.uint8).fill_(0x5a)
     assert (room == 0x5a).all()
+
+
+def test_gates_far_below_zero(fp4):
+    """silu(g) as far down as binary32 has e^-g and its reciprocal, in the products that a large `up` makes of it; 0 beyond; the type's lowest value too."""
+    g = torch.cat([-torch.linspace(60, 87, 128), -torch.linspace(89, 200, 126), torch.tensor([-3.3e38, -1e4])]).to(torch.bfloat16)
+    g = torch.where(g < -88.5, g, g.clamp(min=-87.0))
+    x = torch.cat([g, torch.full((256,), 1e30).to(torch.bfloat16)])[None].cuda()
+    codes, scales = fp4.fp8_quantize(x, flags=fp4.SILU_MUL)
+    v = R.f64(x[:, :256])
+    v, delta = v / (1 + np.exp(-np.maximum(v, -600.0))) * R.f64(x[:, 256:]), (1.5 * np.minimum(np.abs(v), 128.0) + 8) * 2 * U
+    R.check_operand(codes[:, :128], scales[:, :1], v[:, :128], delta[:, :128])
+    assert (codes.float()[:, 128:] == 0).all() and (scales[:, 1] == 2.0 ** -100 / 448).all()
+    x[0, 3] = -float("inf")
+    assert torch.isnan(fp4.fp8_quantize(x, flags=fp4.SILU_MUL)[1][0, 0])
