@@ -73,7 +73,11 @@ enum {
     FP4MR_W_SCALE43 = 1u << 9,            /* MXFP4 products: the W operand was quantized with SCALE_ROUND43   */
     FP4MR_SCALE_FIT_TENSOR = 1u << 10,    /* NVFP4 quantize ops, with SCALE_MSE: also fit the tensor scale    */
     FP4MR_SCALE_FIT_RANGE = 1u << 11,     /* MXFP4 quantize ops: scale byte fitted to the tensor's range (below) */
-    FP4MR_SILU_MUL = 1u << 12             /* fp8_quantize: quantize silu(gate) * up of rows [gate | up]       */
+    FP4MR_SILU_MUL = 1u << 12,            /* fp8_quantize, int8_quantize: quantize silu(gate) * up of rows [gate | up] */
+    FP4MR_ROUTE_SIGMOID = 1u << 13,       /* moe_route: scores are sigmoid(logit), not the softmax of a token's logits */
+    FP4MR_ROUTE_RENORM = 1u << 14,        /* moe_route: a token's weights are divided by their sum            */
+    FP4MR_ROUTE_GROUP_SUM2 = 1u << 15,    /* moe_route: a group counts as the sum of its two best, not as its best */
+    FP4MR_SHARED_F32 = 1u << 16           /* moe_combine: shared is fp32, not bf16                            */
 };
 
 /* operation selector for fp4_workspace_bytes */
@@ -427,6 +431,78 @@ size_t fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, uint32_t flags);
 fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int64_t a_rows, const void* w_codes, const float* w_scales,
                                 const int32_t* offsets, const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K,
                                 void* out, uint32_t flags, void* stream);
+
+/*
+ * The integer form of those layers: codes -128 .. 127 with one fp32 scale per row, that is, per token of the activations (codes [M,K], scales [M]) and per
+ * channel of the weights (codes [N,K], scales [N]; of several experts [E,N,K] and [E,N]), all row-major and contiguous.  An operand stands for  code * scale.  The quantizers write
+ *   scale = max(amax, 2^-100) / 127 ,  code = the integer nearest to  v * (127 * (1 / max(amax, 2^-100))) , ties to even ,
+ * with amax the row's largest |v|, every operation in binary32 (of a bf16 tensor as it is, the code of the exact quotient 127 v / amax; one in the middle of two codes may be either); codes are -127 .. 127.  A row that holds a NaN or an infinity has
+ * a scale that is not finite, and every output of a product that reads it is NaN or infinite.
+ * K is a multiple of 16 in all calls and at most FP4MR_INT8_MAX_K (FP4MR_ERR_SHAPE), so that a sum of K products of any codes has 32 bits; M and N are any sizes; M, N <= 2^24 (M of int8_quantize 2^31), in products
+ * M N <= 2^38.  No rows (M, or rows, of 0) is not an error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.  Scales, and the outputs of products, need the alignment of their
+ * elements only.
+ *
+ * int8_rmsnorm_quantize and int8_quantize: arguments as fp8_rmsnorm_quantize and fp8_quantize have them (x_stride a multiple of 8; K of the norm <= 65536); scales_out [M].  Weights are quantized by
+ * int8_quantize, their channels (of all experts) being its rows.
+ */
+#define FP4MR_INT8_MAX_K 131056
+fp4mr_status_t int8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t M, int64_t K,
+                                     float eps, void* codes_out, float* scales_out, void* residual_out, void* norm_out,
+                                     uint32_t flags, void* stream);
+fp4mr_status_t int8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t K, void* codes_out, float* scales_out, uint32_t flags,
+                             void* stream);
+
+/*
+ * out[m,n] = (float(sum_k a[m,k] w[n,k]) * a_scales[m]) * w_scales[n]: the sum is exact, float() rounds it to the nearest binary32, and both multiplications are binary32's.  out is bf16
+ * (one more rounding), or fp32 with FP4MR_OUT_F32.  No plan, workspace or kernel changes a bit of it.
+ *   workspace    optional: with int8_workspace_bytes(M, N, K) bytes (0 where that is of no use) a product of few tiles and a long K is split along K over otherwise
+ *                idle compute units, and its parts' sums are kept there.  With less, or NULL, it runs in fewer parts, or in one.
+ */
+fp4mr_status_t int8_gemm(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales, int64_t M, int64_t N,
+                         int64_t K, void* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+size_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/* The same with rows grouped by expert: offsets, index and the rest as fp8_grouped_gemm has them (an index outside A stands for a row of zeros with a scale of zero). */
+fp4mr_status_t int8_grouped_gemm(const void* a_codes, const float* a_scales, int64_t a_rows, const void* w_codes, const float* w_scales,
+                                 const int32_t* offsets, const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K,
+                                 void* out, uint32_t flags, void* stream);
+
+/*
+ * A router's choice: from the logits of T tokens to each one's `top` experts with their weights, and to the rows by expert that the grouped products take.
+ *   s[t,e] = softmax over e of logits[t,:], or sigmoid(logits[t,e]) with FP4MR_ROUTE_SIGMOID;   c[t,e] = logits[t,e], or s[t,e] + bias[e] where there is a bias
+ *   groups       the experts are so many runs of experts / groups; a run counts as its largest c, or with FP4MR_ROUTE_GROUP_SUM2 as the sum of its two largest (c = s then, also without a
+ *                bias; a run of one counts as it); only the experts of the top_groups best runs may be chosen
+ *   the choice   the `top` largest c, in descending order; of equal ones, runs and experts alike, the lower index.  Where a score enters c, c is formed in binary64, else the logits are compared as they are.
+ *   weights      scale * s of the chosen, or with FP4MR_ROUTE_RENORM scale * s / max(sum of the chosen s, 2^-100); the bias has no part in them; within 2^-20 of the value
+ * A logit or bias of minus infinity takes an expert out.  A token with fewer than `top` experts left has experts -1, weights 0 and places -1 behind them; one with none (a row of padding, masked whole) has no rows
+ * at all.  A token with a NaN among its logits or the biases, or with softmax an infinite logit, has no rows either, and all its weights are NaN.
+ *   logits       bf16 (fp32 with FP4MR_INPUT_F32), rows of `experts` elements logits_stride elements apart
+ *   bias         fp32 [experts] or NULL
+ *   weights_out  fp32 [T,top]
+ *   experts_out  int32 [T,top]
+ *   rows_out     int32, room for [T * top]: the token of each row, the rows of expert 0 first, an expert's in the order of the tokens.  What lies behind the last row is not written.
+ *   offsets_out  int32 [experts + 1]: expert e has rows offsets[e] .. offsets[e+1] - 1
+ *   places_out   int32 [T,top]: the row of each choice, -1 where there is none
+ *   workspace    moe_workspace_bytes(T, experts, top) bytes, 16-byte aligned
+ * T <= 2^24, T * top <= 2^30, experts <= 1024, top <= 64 and <= experts / groups * top_groups, groups <= 64 and a divisor of experts.  Tensors need the alignment of their elements only.  T = 0 writes offsets_out.
+ * Outputs must not overlap inputs or each other.
+ */
+fp4mr_status_t moe_route(const void* logits, int64_t logits_stride, const float* bias, int64_t T, int64_t experts, int64_t top,
+                         int64_t groups, int64_t top_groups, float scale, float* weights_out, int32_t* experts_out, int32_t* rows_out,
+                         int32_t* offsets_out, int32_t* places_out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+size_t moe_workspace_bytes(int64_t T, int64_t experts, int64_t top);
+
+/*
+ * The rows of the experts back to their tokens:  out[t,:] = shared[t,:] + sum_j weights[t,j] * y[places[t,j],:],  in fp32, added in the order of j.
+ *   y            bf16 (fp32 with FP4MR_INPUT_F32) [y_rows, cols]
+ *   places       int32 [T,top]; one outside 0 .. y_rows - 1 adds its weight times zero (0, or NaN)
+ *   weights      fp32 [T,top]
+ *   shared       bf16 (fp32 with FP4MR_SHARED_F32) [T,cols], or NULL
+ *   out          bf16 (fp32 with FP4MR_OUT_F32) [T,cols]; may be shared itself where both have one type, else must not overlap an input
+ * T <= 2^24, T * top and y_rows <= 2^30, top <= 64, cols <= 2^24 and any number; T = 0 launches nothing.  Tensors need the alignment of their elements only (faster where all rows are 16-byte aligned).
+ */
+fp4mr_status_t moe_combine(const void* y, int64_t y_rows, const int32_t* places, const float* weights, const void* shared, int64_t T,
+                           int64_t top, int64_t cols, void* out, uint32_t flags, void* stream);
 
 /* Bytes of device scratch the given operation needs (0 = none).  rows = M for the quantize ops. */
 size_t fp4_workspace_bytes(int op, int64_t M, int64_t N, int64_t K, fp4mr_fmt_t fmt, uint32_t flags);

@@ -33,6 +33,10 @@ SCALE_FIT_TENSOR = 1 << 10
 SCALE_FIT_RANGE = 1 << 11
 FIT_RANGE_FLOATS = 258
 SILU_MUL = 1 << 12
+ROUTE_SIGMOID = 1 << 13
+ROUTE_RENORM = 1 << 14
+ROUTE_GROUP_SUM2 = 1 << 15
+SHARED_F32 = 1 << 16
 A_SCALE43 = 1 << 8
 W_SCALE43 = 1 << 9
 OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC, OPT_FP8_VARIANT = 0, 1, 2, 3
@@ -83,6 +87,22 @@ lib.fp8_workspace_bytes.restype = _sz
 lib.fp8_gemm.restype = _i32
 lib.fp8_grouped_gemm.argtypes = [_p, _p, _i64, _p, _p, _p, _p, _i64, _i64, _i64, _i64, _p, _u32, _p]
 lib.fp8_grouped_gemm.restype = _i32
+lib.int8_rmsnorm_quantize.argtypes = lib.fp8_rmsnorm_quantize.argtypes
+lib.int8_rmsnorm_quantize.restype = _i32
+lib.int8_quantize.argtypes = lib.fp8_quantize.argtypes
+lib.int8_quantize.restype = _i32
+lib.int8_gemm.argtypes = lib.fp8_gemm.argtypes
+lib.int8_gemm.restype = _i32
+lib.int8_workspace_bytes.argtypes = [_i64, _i64, _i64]
+lib.int8_workspace_bytes.restype = _sz
+lib.int8_grouped_gemm.argtypes = lib.fp8_grouped_gemm.argtypes
+lib.int8_grouped_gemm.restype = _i32
+lib.moe_route.argtypes = [_p, _i64, _p, _i64, _i64, _i64, _i64, _i64, ctypes.c_float, _p, _p, _p, _p, _p, _p, _sz, _u32, _p]
+lib.moe_route.restype = _i32
+lib.moe_workspace_bytes.argtypes = [_i64, _i64, _i64]
+lib.moe_workspace_bytes.restype = _sz
+lib.moe_combine.argtypes = [_p, _i64, _p, _p, _p, _i64, _i64, _i64, _p, _u32, _p]
+lib.moe_combine.restype = _i32
 lib.fp4_set_option.argtypes = [_i32, _i32]
 lib.fp4_set_option.restype = _i32
 
@@ -483,6 +503,163 @@ def fp8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=None
     out, N, K = _product_out(a_codes, a_scales, w_codes, w_scales, 3, T, flags, out)
     _check(lib.fp8_grouped_gemm(a_codes.data_ptr(), a_scales.data_ptr(), a_codes.shape[0], w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), _ptr(rows),
                                 T, E, N, K, out.data_ptr(), flags, _stream()))
+    return out
+
+
+# ---- the integer form of the 8-bit layers: codes (torch.int8) with a float32 scale per row: per token of the activations (codes [M,K], scales [M]), per channel of
+# the weights (codes [N,K], scales [N], or with experts in front).  These calls and the router's take their tensors from the current device.
+INT8_MAX_K = 131056
+
+
+def _new(like, shape, dtype):
+    return (like.new_empty if type(like) is _Tensor else _plain_empty(like))(shape, dtype=dtype)
+
+
+def _is_tensor(t, dtype, *shape):
+    """A contiguous tensor on the current device."""
+    assert t.is_cuda and t.device.index == _current_device() and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == shape
+
+
+def _is_operand8i(codes, scales, *shape):
+    _is_tensor(codes, torch.int8, *shape)
+    _is_tensor(scales, torch.float32, *shape[:-1])
+
+
+def int8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residual_out=None, norm_out=None, codes=None, scales=None):
+    """codes, scales, h = Q(v) with v = h * weight / sqrt(mean(h^2) + eps) and h = bf16(x + residual), or x (then the third result is None).
+    x: bf16 [M,K], rows may be apart (K % 16 == 0, K <= 65536); weight: bf16 [K]; residual: bf16 [M,K].  residual_out: where h goes (may be residual
+    or x themselves, a new tensor if None); norm_out: bf16 [M,K] to receive v too."""
+    M, K, stride = _rows(x)
+    assert x.device.index == _current_device()
+    _is_tensor(weight, torch.bfloat16, K)
+    if residual is not None and residual_out is None:
+        residual_out = _new(x, (M, K), torch.bfloat16)
+    for t in (residual, residual_out, norm_out):
+        if t is not None:
+            _is_tensor(t, torch.bfloat16, M, K)
+    codes = _new(x, (M, K), torch.int8) if codes is None else codes
+    scales = _new(x, (M,), torch.float32) if scales is None else scales
+    _is_operand8i(codes, scales, M, K)
+    _check(lib.int8_rmsnorm_quantize(x.data_ptr(), stride, _ptr(residual), weight.data_ptr(), M, K, eps, codes.data_ptr(), scales.data_ptr(), _ptr(residual_out),
+                                     _ptr(norm_out), 0, _stream()))
+    return codes, scales, residual_out
+
+
+def int8_quantize(x, *, flags: int = 0, codes=None, scales=None):
+    """codes, scales = Q(x), a scale per row, of bf16 activations [M,K] (rows may be apart), or with SILU_MUL of silu(x[:, :K]) * x[:, K:] of x [M, 2K]; of weights [N,K], or of
+    experts [E,N,K] (contiguous).  K % 16 == 0."""
+    if x.dim() == 3:
+        assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous()
+        M, K, stride = x.shape[0] * x.shape[1], x.shape[2], x.shape[2]
+    else:
+        M, K, stride = _rows(x)
+    assert x.device.index == _current_device()
+    if flags & SILU_MUL:
+        assert K % 2 == 0
+        K //= 2
+    shape = (*x.shape[:-1], K)
+    codes = _new(x, shape, torch.int8) if codes is None else codes
+    scales = _new(x, shape[:-1], torch.float32) if scales is None else scales
+    _is_operand8i(codes, scales, *shape)
+    _check(lib.int8_quantize(x.data_ptr(), stride, M, K, codes.data_ptr(), scales.data_ptr(), flags, _stream()))
+    return codes, scales
+
+
+def _product8i_out(a_codes, a_scales, w_codes, w_scales, dim: int, rows: int, flags: int, out):
+    assert a_codes.dim() == 2 and w_codes.dim() == dim
+    N, K = w_codes.shape[-2:]
+    _is_operand8i(a_codes, a_scales, a_codes.shape[0], K)
+    _is_operand8i(w_codes, w_scales, *w_codes.shape)
+    dtype = torch.float32 if flags & OUT_F32 else torch.bfloat16
+    out = _new(a_codes, (rows, N), dtype) if out is None else out
+    _is_tensor(out, dtype, rows, N)
+    return out, N, K
+
+
+def int8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None, workspace=None):
+    """out[M,N] = A W^T (bf16, or fp32 with OUT_F32) from the int8 codes and row scales of activations [M,K] and weights [N,K]; the sums are exact."""
+    M = a_codes.shape[0]
+    out, N, K = _product8i_out(a_codes, a_scales, w_codes, w_scales, 2, M, flags, out)
+    need = int8_workspace_bytes(M, N, K)
+    if need and workspace is None:
+        workspace = _new(a_codes, (need,), torch.uint8)
+    assert workspace is None or (workspace.is_cuda and workspace.device == a_codes.device and workspace.is_contiguous())
+    wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.int8_gemm(a_codes.data_ptr(), a_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), M, N, K, out.data_ptr(), _ptr(workspace), wsz, flags, _stream()))
+    return out
+
+
+def int8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.int8_workspace_bytes(M, N, K))
+
+
+def int8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=None, flags: int = 0, out=None):
+    """Rows offsets[e] .. offsets[e+1] - 1 of out = those rows of A times the weights of expert e, w_codes [E,N,K]; offsets: int32 [E+1].
+    rows: int32 [T], the row of A for each row of out (outside A: a row of zeros); without it out has A's rows.  Rows of out that no expert has are
+    not written (a new out holds what its memory held)."""
+    _is_tensor(offsets, torch.int32, w_codes.shape[0] + 1)
+    T = a_codes.shape[0]
+    if rows is not None:
+        T = rows.shape[0]
+        _is_tensor(rows, torch.int32, T)
+    out, N, K = _product8i_out(a_codes, a_scales, w_codes, w_scales, 3, T, flags, out)
+    _check(lib.int8_grouped_gemm(a_codes.data_ptr(), a_scales.data_ptr(), a_codes.shape[0], w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), _ptr(rows),
+                                 T, w_codes.shape[0], N, K, out.data_ptr(), flags, _stream()))
+    return out
+
+
+# ---- a router's choice of experts, and their outputs added up
+def moe_workspace_bytes(T: int, experts: int, top: int) -> int:
+    return int(lib.moe_workspace_bytes(T, experts, top))
+
+
+def moe_route(logits, top: int, *, bias=None, groups: int = 1, top_groups: int = 1, scale: float = 1.0, flags: int = 0, workspace=None):
+    """weights, experts, rows, offsets, places from the logits [T,E] of a router (bf16 or float32; rows may be apart): each token's `top` best experts (int32 [T,top], in descending
+    order, equal ones by index) and their weights (float32), and the rows by expert that the grouped products take: the token of each row (int32 [T*top]), where each expert's begin
+    (int32 [E+1]), and each choice's row (int32 [T,top]).  flags: ROUTE_SIGMOID (scores; else softmax), ROUTE_RENORM (weights divided by their sum), ROUTE_GROUP_SUM2.  bias: float32 [E],
+    added to the scores for the choice alone.  groups, top_groups: only the experts of the best groups may be chosen.  An expert of -inf is not chosen; a choice that a token does
+    not have is -1, with a weight of 0 and a place of -1, and has no row (rows behind offsets[E] are not written)."""
+    assert logits.is_cuda and logits.device.index == _current_device() and logits.dim() == 2 and logits.dtype in (torch.bfloat16, torch.float32)
+    T, E = logits.shape
+    assert logits.stride(1) == 1 or E <= 1
+    stride = logits.stride(0) if T > 1 else E
+    if logits.dtype == torch.float32:
+        flags |= INPUT_F32
+    if bias is not None:
+        _is_tensor(bias, torch.float32, E)
+    assert 0 < top <= E
+    weights, experts, places = _new(logits, (T, top), torch.float32), _new(logits, (T, top), torch.int32), _new(logits, (T, top), torch.int32)
+    rows, offsets = _new(logits, (T * top,), torch.int32), _new(logits, (E + 1,), torch.int32)
+    need = moe_workspace_bytes(T, E, top)
+    if need and workspace is None:
+        workspace = _new(logits, (need,), torch.uint8)
+    assert workspace is None or (workspace.is_cuda and workspace.device == logits.device and workspace.is_contiguous())
+    wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.moe_route(logits.data_ptr(), stride, _ptr(bias), T, E, top, groups, top_groups, scale, weights.data_ptr(), experts.data_ptr(), rows.data_ptr(), offsets.data_ptr(),
+                         places.data_ptr(), _ptr(workspace), wsz, flags, _stream()))
+    return weights, experts, rows, offsets, places
+
+
+def moe_combine(y, places, weights, *, shared=None, flags: int = 0, out=None):
+    """out[T,H] = shared + sum over j of weights[:, j] * y[places[:, j]], in float32 and rounded once (bf16, or float32 with OUT_F32).  y: bf16 or float32 [rows,H]; places: int32 [T,top]
+    (outside y: the weight times zero); weights: float32 [T,top]; shared: bf16 or float32 [T,H] (may be out)."""
+    assert y.dim() == 2 and places.dim() == 2 and y.dtype in (torch.bfloat16, torch.float32)
+    R, H = y.shape
+    T, top = places.shape
+    _is_tensor(y, y.dtype, R, H)
+    _is_tensor(places, torch.int32, T, top)
+    _is_tensor(weights, torch.float32, T, top)
+    if y.dtype == torch.float32:
+        flags |= INPUT_F32
+    if shared is not None:
+        assert shared.dtype in (torch.bfloat16, torch.float32)
+        _is_tensor(shared, shared.dtype, T, H)
+        if shared.dtype == torch.float32:
+            flags |= SHARED_F32
+    dtype = torch.float32 if flags & OUT_F32 else torch.bfloat16
+    out = _new(y, (T, H), dtype) if out is None else out
+    _is_tensor(out, dtype, T, H)
+    _check(lib.moe_combine(y.data_ptr(), R, places.data_ptr(), weights.data_ptr(), _ptr(shared), T, top, H, out.data_ptr(), flags, _stream()))
     return out
 
 

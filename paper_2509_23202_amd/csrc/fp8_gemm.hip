@@ -11,8 +11,7 @@
 // m, and the one activation scale.  Both operands are row-major, 128 bytes of a row to a step: lane l reads row l % 16, and from the row's
 // eight pieces of 16 bytes the pieces l / 16 and l / 16 + 4 (the product does not care which of the 128 k is which, as long as both
 // operands agree).
-#include "device_util.hpp"
-#include "internal.hpp"
+#include "product_tiles.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -68,88 +67,7 @@ __device__ __forceinline__ v4f mfma_fp8(const v4i (&a)[2], const v4i (&b)[2])
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
 }
 
-struct Rows {
-    int expert, begin, end;    // rows begin .. end - 1 of the output; none: begin == end
-};
-
-// Rows of expert base + lane, kept within the output whatever the offsets hold, and the inclusive sum over the lanes of their tiles of R rows.
-struct ExpertTiles {
-    int lo, hi, upto;
-};
-__device__ __forceinline__ ExpertTiles expert_tiles(const Fp8Args& g, int base, int R)
-{
-    const int e = base + ((int)threadIdx.x & 63), at = min(e, g.experts - 1), T = (int)g.rows;
-    const int begin = g.offsets[at], end = g.offsets[at + 1];
-    ExpertTiles x;
-    x.lo = min(max(begin, 0), T);
-    x.hi = min(max(end, x.lo), T);
-    int n = e < g.experts ? (x.hi - x.lo + R - 1) / R : 0;
-    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8: the sum within sixteen lanes
-    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, true);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, true);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, true);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);    // row_bcast 15 to the second and fourth sixteen, row_bcast 31 to the second half
-    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
-    x.upto = n;
-    return x;
-}
-
-// Tiles of R rows of all experts: tiles never span experts, and those of an expert follow one another.  Offsets that do not decrease make `most` at most.
-// first: of the first 64 experts.
-__device__ __forceinline__ int count_tiles(const Fp8Args& g, const ExpertTiles& first, int R, int most)
-{
-    int n = min(__builtin_amdgcn_readlane(first.upto, 63), most);
-    for (int base = 64; base < g.experts; base += 64) n = min(n + __builtin_amdgcn_readlane(expert_tiles(g, base, R).upto, 63), most);
-    return n;
-}
-
-__device__ __forceinline__ Rows find_tile(const Fp8Args& g, const ExpertTiles& first, int tile, int R)
-{
-    ExpertTiles x = first;
-    for (int base = 0, before = 0;;) {
-        const uint64_t here = __ballot(tile < before + x.upto);
-        if (here) {
-            const int l = __builtin_ctzll(here), earlier = l ? __builtin_amdgcn_readlane(x.upto, l - 1) : 0;
-            const int begin = __builtin_amdgcn_readlane(x.lo, l) + (tile - before - earlier) * R;
-            return Rows{base + l, begin, min(begin + R, __builtin_amdgcn_readlane(x.hi, l))};
-        }
-        before += __builtin_amdgcn_readlane(x.upto, 63);
-        base += 64;
-        if (base >= g.experts) return Rows{0, 0, 0};
-        x = expert_tiles(g, base, R);
-    }
-}
-
-constexpr uint32_t kOutside = (uint32_t)kFp8MaxGathered;    // an offset past every operand, to which K may be added
 constexpr uint32_t kPast = 0x08000000u;       // past all activations' scales (4 / 128 of kOutside), and kOutside may be added
-
-// What the pieces of a row are exchanged by: the sixteen rows of a fragment, which lie next to each other (X) or four by four, sixteen apart (W), have every
-// pair of key and row % 2 once.
-__device__ __forceinline__ int x_key(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int w_key(int row) { return ((row >> 1) & 1) | (row / 16 & 3) << 1; }
-
-// A copy of a lane's number that the compiler takes for another one: what is computed from it stays where it is needed, once a tile, instead of in registers
-// throughout the main loop.
-__device__ __forceinline__ int kept_here(int lane)
-{
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
-
-// 16 or 4 bytes of every lane to LDS, the lanes' one behind the other from `to`
-typedef __attribute__((address_space(3))) char lds_char;
-__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t from, char* smem, int to, uint32_t offset, int uniform_offset)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)((lds_char*)smem + to), 16, offset, uniform_offset, 0, 0);
-}
-__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, char* smem, int to, uint32_t offset)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)((lds_char*)smem + to), 4, offset, 0, 0, 0);
-}
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)(bytes > 0xffffffffll ? 0xffffffffu : (uint32_t)bytes), 0x00020000);
-}
 
 // ---------------------------------------------------------------- few rows: weights streamed from memory
 // 16 TN columns and 16 TM rows to a tile; a workgroup walks a run of tiles.  Its waves share K, each with a run of blocks; a block's codes and scales go to the
@@ -377,17 +295,6 @@ struct Tile {
     static constexpr bool ROLLED = TM >= 8;    // (see the kernel)
     static_assert(S == (ROLLED ? 2 : 4) && (S - 1) * LPS < 64, "");
 };
-
-// Workgroups are dealt round-robin to the eight XCDs: each gets one contiguous range of tiles, in bands of four rows of tiles, so that those that share an
-// L2 share operands.
-__device__ __forceinline__ void place(int bid, int n, int tiles_m, int tiles_n, int& tm, int& tn)
-{
-    const int per = n >> 3, rem = n & 7, xcd = bid & 7, idx = bid >> 3;
-    const int at = xcd < rem ? xcd * (per + 1) + idx : rem * (per + 1) + (xcd - rem) * per + idx;
-    const int band = 4 * tiles_n, first = at / band * 4, high = min(tiles_m - first, 4), in = at % band;
-    tm = first + in % high;
-    tn = in / high;
-}
 
 // EXACT: fp32 sums (the fp16 MFMA); OUT_F32: they leave as fp32.  SPLIT: a unit of work is one part of K of a tile, each of part_blocks blocks but the last, and
 // what leaves is its sums, to the part's own copy of the output.

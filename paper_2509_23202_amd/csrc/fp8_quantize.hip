@@ -7,48 +7,13 @@
 // asks for).  2^-100 keeps the reciprocal finite and gives a block of zeros the code 0 and a finite scale.  amax is an integer maximum
 // of the magnitudes' bit patterns, which orders infinity above every number and NaN above that: a block that holds one has the scale
 // infinity or NaN, and every product with it is NaN.
-#include "device_util.hpp"
+#include "bf16_rows.hpp"
 #include "internal.hpp"
 
 namespace fp4mr {
 namespace {
 
 constexpr float kE4m3Max = 448.0f;
-constexpr uint32_t kAmaxLeast = 27u << 23;   // 2^-100
-
-typedef __bf16 v8b __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ void widen8(const v4i& raw, float (&v)[8])
-{
-    const v8b t = __builtin_bit_cast(v8b, raw);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
-}
-
-// STREAM: read once, past the caches' interest
-template <bool STREAM>
-__device__ __forceinline__ v4i load16(const __bf16* p)
-{
-    const v4i* const q = reinterpret_cast<const v4i*>(p);
-    if constexpr (STREAM) return __builtin_nontemporal_load(q);
-    else return *q;
-}
-
-__device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
-{
-    v8b t;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = (__bf16)v[i];
-    __builtin_nontemporal_store(__builtin_bit_cast(v4i, t), reinterpret_cast<v4i*>(p));
-}
-
-__device__ __forceinline__ uint32_t amax8(const float (&v)[8])
-{
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    return m;
-}
 
 // Largest value among the sixteen lanes that hold a block of 128, in all of them.
 __device__ __forceinline__ uint32_t max16(uint32_t m)
@@ -75,12 +40,6 @@ __device__ __forceinline__ void quantize8(const float (&v)[8], uint8_t* codes, f
     const float amax = __uint_as_float(max(max16(amax8(v)), kAmaxLeast));
     *reinterpret_cast<v2i*>(codes) = codes8(v, kE4m3Max / amax);
     if ((lane & 15) == 0) *scale = amax / kE4m3Max;
-}
-
-// silu(gate) * up
-__device__ __forceinline__ float silu_mul(float g, float u)
-{
-    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
 }
 
 struct QuantArgs {

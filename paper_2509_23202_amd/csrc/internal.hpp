@@ -178,9 +178,28 @@ size_t fp8_gemm_partial_bytes(int64_t M, int64_t N, int64_t K, bool out_f32);
 hipError_t launch_fp8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
                            void* partial, size_t room, hipStream_t st);
 // with an index a_rows * K <= kFp8MaxGathered: the kernels' offsets have 32 bits
-constexpr int64_t kFp8MaxGathered = 0xf0000000ll;
+constexpr int64_t kFp8MaxGathered = 0xf0000000ll, kMaxGathered = kFp8MaxGathered;
 hipError_t launch_fp8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
+
+// 8-bit integer operands (codes, an fp32 scale per row): shapes and alignment as the C-ABI layer has checked them, K % 16 == 0
+hipError_t launch_int8_quantize(const void* x, int64_t x_stride, int64_t rows, int64_t K, bool silu, void* codes, float* scales, hipStream_t st);
+constexpr int64_t kInt8NormMaxK = 65536;
+hipError_t launch_int8_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, const void* weight, int64_t rows, int64_t K, float eps,
+                                        void* codes, float* scales, void* residual_out, void* norm_out, hipStream_t st);
+// partial: room for the sums of parts of K (int8_gemm_partial_bytes: what the best plan takes; with less another one)
+size_t int8_gemm_partial_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_int8_gemm(const void* a, const float* a_scales, const void* w, const float* w_scales, int64_t M, int64_t N, int64_t K, void* out, bool out_f32,
+                            void* partial, size_t room, hipStream_t st);
+hipError_t launch_int8_grouped_gemm(const void* a, const float* a_scales, int64_t a_rows, const void* w, const float* w_scales, const int32_t* offsets,
+                                    const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
+
+// a router's choices and the rows by expert; counts: moe_count_bytes bytes of scratch
+size_t moe_count_bytes(int64_t tokens, int64_t experts);
+hipError_t launch_moe_route(const void* logits, int64_t stride, bool f32, const float* bias, int64_t tokens, int64_t experts, int64_t top, int64_t groups, int64_t top_groups, float scale,
+                            bool sigmoid, bool renorm, bool sum2, float* weights, int32_t* chosen, int32_t* offsets, int32_t* rows, int32_t* places, void* counts, hipStream_t st);
+hipError_t launch_moe_combine(const void* y, int64_t y_rows, bool y_f32, const int32_t* places, const float* weights, const void* shared, bool shared_f32, int64_t tokens, int64_t top,
+                              int64_t cols, void* out, bool out_f32, hipStream_t st);
 
 hipError_t launch_probe(int which, void* buf, size_t bytes, int iters, hipStream_t st);
 
