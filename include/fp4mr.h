@@ -340,7 +340,7 @@ fp4mr_status_t fp4_dequantize(const void* codes, const void* scales, const float
  *   FP4MR_OPT_FP8_VARIANT   0 (default): fp8_gemm and fp8_grouped_gemm pick their kernel; 1..7: force one of few rows or of tiles, 8..13: fp8_gemm in
  *                           2, 4 or 8 parts of K where the workspace holds their sums (products that a forced kernel does not take run on another)
  */
-enum { FP4MR_OPT_GEMM_VARIANT = 0, FP4MR_OPT_GEMM_GRID = 1, FP4MR_OPT_SW_CODEC = 2, FP4MR_OPT_FP8_VARIANT = 3 };
+enum { FP4MR_OPT_GEMM_VARIANT = 0, FP4MR_OPT_GEMM_GRID = 1, FP4MR_OPT_SW_CODEC = 2, FP4MR_OPT_FP8_VARIANT = 3, FP4MR_OPT_INT8_VARIANT = 4 };
 fp4mr_status_t fp4_set_option(int option, int value);
 
 /*

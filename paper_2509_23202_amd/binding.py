@@ -39,7 +39,7 @@ ROUTE_GROUP_SUM2 = 1 << 15
 SHARED_F32 = 1 << 16
 A_SCALE43 = 1 << 8
 W_SCALE43 = 1 << 9
-OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC, OPT_FP8_VARIANT = 0, 1, 2, 3
+OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC, OPT_FP8_VARIANT, OPT_INT8_VARIANT = 0, 1, 2, 3, 4
 OP_ROTATE_QUANTIZE, OP_QUANTIZE_WEIGHTS, OP_GEMM, OP_GPTQ, OP_GPTQ_PREPARE, OP_GPTQ_HESSIAN, OP_GEMM_SPLIT_K, OP_GEMM_FASTEST = 0, 1, 2, 3, 4, 5, 6, 7
 
 _p, _i64, _i32, _u32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_uint32, ctypes.c_size_t

@@ -161,6 +161,10 @@ fp4mr_status_t fp4_set_option(int option, int value)
             if (value < 0 || value > kMaxFp8Variant) return FP4MR_ERR_FMT;
             o.fp8_variant = value;
             return FP4MR_OK;
+        case FP4MR_OPT_INT8_VARIANT:
+            if (value < 0 || value > kMaxInt8Variant) return FP4MR_ERR_FMT;
+            o.int8_variant = value;
+            return FP4MR_OK;
         default: return FP4MR_ERR_FMT;
     }
 }

@@ -15,6 +15,7 @@ struct Options {
     int gemm_variant = 0;  // 0 = tile shape by the cost model, else a forced tile configuration of the GEMM kernels
     int gemm_grid = 0;     // > 0: cap on the number of persistent workgroups (a small grid walks many tiles each)
     int fp8_variant = 0;   // 0 = by the cost model, else a forced kernel of the 8-bit products
+    int int8_variant = 0;  // 0 = by the cost model, else a forced kernel of the 8-bit integer products
     int sw_codec = 0;      // != 0: element and scale codecs in integer arithmetic instead of the converting instructions
 };
 Options& options();
@@ -41,6 +42,7 @@ int compute_units();
 constexpr int kMaxGemmVariantMx = 18;
 constexpr int kMaxGemmVariantNv = 4;
 constexpr int kMaxFp8Variant = 13;
+constexpr int kMaxInt8Variant = 36;
 // NVFP4: chosen as by itself, but without the kernel that dequantizes both operands in its waves
 constexpr int kVariantNvNoCodes = 4;
 

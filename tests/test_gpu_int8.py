@@ -205,6 +205,53 @@ def test_the_largest_sums_have_32_bits(fp4, M, low):
     assert (out == float(np.float32(low[0] * low[1] * K))).all()
 
 
+KERNELS = list(range(1, 10))
+PARTS = list(range(15, 19)) + list(range(24, 28))
+
+
+@pytest.fixture
+def forced(fp4):
+    """Forces a kernel of the products for one test."""
+    yield lambda kernel: fp4.set_option(fp4.OPT_INT8_VARIANT, kernel)
+    fp4.set_option(fp4.OPT_INT8_VARIANT, 0)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("M,N,K", [(1, 16, 16), (5, 130, 144), (70, 300, 1168), (300, 520, 2064), (33, 1100, 640)])
+def test_every_kernel(fp4, forced, kernel, M, N, K):
+    say(f"int8 kernel {kernel} M={M} N={N} K={K}")
+    forced(kernel)
+    for f32 in (False, True):
+        check_gemm(fp4, M, N, K, f32)
+
+
+@pytest.mark.parametrize("kernel", PARTS)
+@pytest.mark.parametrize("M,N,K", [(70, 300, 3856), (1, 130, 4112), (300, 257, 8192)])
+def test_in_parts_of_k(fp4, forced, kernel, M, N, K):
+    say(f"int8 kernel {kernel} M={M} N={N} K={K}")
+    forced(kernel)
+    for f32 in (False, True):
+        check_gemm(fp4, M, N, K, f32, workspace=torch.full((8 * M * N * 4,), 0xff, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_walk_over_tiles_on_every_kernel(fp4, forced, kernel):
+    """More tiles than workgroups, of a K of one step and of a few: the next tile's loads and scales beside this one's output."""
+    forced(kernel)
+    for M, N, K in ((3000, 5000, 48), (2100, 9000, 400)):
+        say(f"int8 kernel {kernel} M={M} N={N} K={K}")
+        check_gemm(fp4, M, N, K, kernel % 2 == 0)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("gather", [None, 50])
+def test_grouped_on_every_kernel(fp4, forced, kernel, gather):
+    say(f"int8 grouped kernel {kernel} gather={gather}")
+    forced(kernel)
+    grouped(fp4, [70, 0, 3, 129, 0, 300, 64, 257, 1, 40], 1100, 656, kernel, gather)
+    grouped(fp4, [i % 5 for i in range(200)], 72, 512, kernel, gather, f32=True)
+
+
 def grouped(fp4, counts, N, K, seed, gather=None, f32=False):
     E, T = len(counts), sum(counts)
     rows = gather or T
