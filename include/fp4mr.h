@@ -473,7 +473,7 @@ fp4mr_status_t int8_grouped_gemm(const void* a_codes, const float* a_scales, int
  *   groups       the experts are so many runs of experts / groups; a run counts as its largest c, or with FP4MR_ROUTE_GROUP_SUM2 as the sum of its two largest (c = s then, also without a
  *                bias; a run of one counts as it); only the experts of the top_groups best runs may be chosen
  *   the choice   the `top` largest c, in descending order; of equal ones, runs and experts alike, the lower index.  Where a score enters c, c is formed in binary64, else the logits are compared as they are.
- *   weights      scale * s of the chosen, or with FP4MR_ROUTE_RENORM scale * s / max(sum of the chosen s, 2^-100); the bias has no part in them; within 2^-20 of the value
+ *   weights      scale * s of the chosen, or with FP4MR_ROUTE_RENORM scale * s / max(sum of the chosen s, 2^-60); the bias has no part in them; within 2^-20 of the value or 2^-50 of scale
  * A logit or bias of minus infinity takes an expert out.  A token with fewer than `top` experts left has experts -1, weights 0 and places -1 behind them; one with none (a row of padding, masked whole) has no rows
  * at all.  A token with a NaN among its logits or the biases, or with softmax an infinite logit, has no rows either, and all its weights are NaN.
  *   logits       bf16 (fp32 with FP4MR_INPUT_F32), rows of `experts` elements logits_stride elements apart

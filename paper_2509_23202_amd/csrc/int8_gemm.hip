@@ -7,9 +7,6 @@
 // a step: lane l reads row l % 16, and from the row's eight pieces of 16 bytes the pieces l / 16 and l / 16 + 4, one for each of two MFMAs.  What lies past K is
 // zero in W, and may be anything in A.
 #include "product_tiles.hpp"
-#ifndef EARLY_GROUPS
-#define EARLY_GROUPS 3
-#endif
 
 #include <algorithm>
 #include <cmath>
@@ -30,6 +27,8 @@ struct Int8Args {
     const int32_t* index;      // grouped: row of A for a row of the output, or null
     int experts;
 };
+
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(2)));
 
 enum { kBf16, kF32, kSums };   // what leaves: the output in one of its types, or the sums of a part of K
 
@@ -226,34 +225,35 @@ __global__ __launch_bounds__(C::WAVES * 64) void int8_stream_kernel(Int8Args g, 
 //   Two stages: before its last X fragment a wave has read all it needs of the stage.  There it waits for its loads of the next one, the workgroup meets, and the last fragment's products cover the reads of
 // the next step's first fragments.  More stages: a step begins with the meeting.
 //   A tile takes S steps at least: the meeting in a step that is not one of its last S - 1 stands between a tile's output, which reads its scales, and the loads of the scales two tiles on.
-template <int TM_, int TN_, int NWM_, int NWN_, int STAGES_>
+template <int TM_, int TN_, int NWM_, int NWN_, int BK_, int STAGES_, bool EARLY_ = false>
 struct Tile {
-    static constexpr int TM = TM_, TN = TN_, NWM = NWM_, NWN = NWN_, S = STAGES_, NW = NWM * NWN;
-    static constexpr int BM = 16 * TM * NWM, BN = 16 * TN * NWN;
-    static constexpr int STAGE = (BM + BN) * 128, SCALES = (BM + BN) * 4;
-    static constexpr int XL = BM / 8 / NW, WL = BN / 8 / NW, LPS = XL + WL;   // loads of a wave for a step: X, W
+    static constexpr int TM = TM_, TN = TN_, NWM = NWM_, NWN = NWN_, BK = BK_, S = STAGES_, NW = NWM * NWN;
+    static constexpr bool EARLY = EARLY_;
+    static constexpr int BM = 16 * TM * NWM, BN = 16 * TN * NWN, EACH = 1024 / BK;     // EACH: rows to a load
+    static constexpr int STAGE = (BM + BN) * BK, SCALES = (BM + BN) * 4;
+    static constexpr int XL = BM / EACH / NW, WL = BN / EACH / NW, LPS = XL + WL;      // loads of a wave for a step: X, W
     static constexpr int kScales = S * STAGE;                                 // of two tiles in turn
     static constexpr int kRoom = kScales + 2 * SCALES, ROOM = 512 * TN;       // for the output, of each wave
     static constexpr int lds() { return kRoom + NW * ROOM; }
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && S >= 2 && (S - 1) * LPS < 64 && lds() <= 163840, "");
+    // What the pieces of a row are exchanged by, so that the sixteen rows of a fragment (of W: four in each of four runs of 4 TN) have every pair of key and place within 256 bytes once.
+    static __device__ __forceinline__ int x_key(int row) { return BK == 128 ? row >> 1 & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int w_key(int row) { return BK == 128 ? (row >> 1 & 1) | (row / (4 * TN) & 3) << 1 : row / (4 * TN) & 3; }
+    static_assert((BK == 64 || BK == 128) && BM % (EACH * NW) == 0 && BN % (EACH * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && S >= (EARLY ? 3 : 2) && (S - 1) * LPS < 64 && lds() <= 163840, "");
 };
 
-// What the pieces of a row of W are exchanged by: a fragment has four rows in each of four runs of 4 TN.
-template <int TN>
-__device__ __forceinline__ int w_key_of(int row) { return ((row >> 1) & 1) | (row / (4 * TN) & 3) << 1; }
-
-// split_parts: a unit of work is one part of K of a tile, each of split_steps steps but the last, and what leaves (OUT = kSums) is its sums, to the part's own copy of the output.
+// split_parts: a unit of work is one part of K of a tile, each of split_blocks times 128 columns but the last, and what leaves (OUT = kSums) is its sums, to the part's own copy of the output.
 template <bool GROUPED, int OUT, typename C>
-__global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int tiles_m, int tiles_n, int split_parts, int split_steps)
+__global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int tiles_m, int tiles_n, int split_parts, int split_blocks)
 {
     constexpr bool SPLIT = OUT == kSums;
     static_assert(!SPLIT || !GROUPED, "");
     constexpr int TM = C::TM, TN = C::TN, NW = C::NW, S = C::S, LPS = C::LPS;
-    constexpr bool EARLY = S > 2;
+    constexpr int BK = C::BK, H = BK / 64;      // H: MFMAs along a stage
+    constexpr bool EARLY = C::EARLY;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave % C::NWM, wn = wave / C::NWM;
-    const int K = (int)g.K, KB = (K + 127) >> 7, parts = SPLIT ? split_parts : 1;
+    const int K = (int)g.K, parts = SPLIT ? split_parts : 1;
     const bool gather = GROUPED && g.index != nullptr;
     if constexpr (GROUPED) tiles_m = count_tiles(g, expert_tiles(g, 0, C::BM), C::BM, tiles_m);
     const int ntiles = tiles_m * tiles_n * parts;
@@ -266,17 +266,14 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
     __amdgpu_buffer_rsrc_t rx, rw;
     uint32_t xo[C::XL], wo[C::WL];
     int t = 0;                 // the step whose loads go out
-    // piece of a row of W that the lane loads with the i-th load: its own, exchanged by the key
-    const int w_piece = (lane & 7) ^ ((lane >> 4) & 1);
-    auto w_run = [&](int i) { return (i * NW + wave) * 8 / (4 * TN) & 3; };        // (the eight rows of a load lie in one run)
     auto issue = [&](int stage, int i) {
-        const int at = k_first + t * 128;
+        const int at = k_first + t * BK;
         if (i < C::XL) {
             load_lds16(rx, smem, stage + (i * NW + wave) * 1024, xo[i < C::XL ? i : 0], at);
         } else {
-            const int j = i - C::XL, q = j >= 0 && j < C::WL ? j : 0;
-            const uint32_t past = at + (w_piece ^ (w_run(q) << 1)) * 16 < K ? 0u : kOutside;
-            load_lds16(rw, smem, stage + C::BM * 128 + (q * NW + wave) * 1024, wo[q] | past, at);
+            const int q = i - C::XL, j = q >= 0 && q < C::WL ? q : 0;
+            const int n = (j * NW + wave) * C::EACH + lane / (BK / 16), piece = (lane % (BK / 16)) ^ C::w_key(n);
+            load_lds16(rw, smem, stage + C::BM * BK + (j * NW + wave) * 1024, wo[j] | (at + piece * 16 < K ? 0u : kOutside), at);
         }
     };
     // In front of a tile's first codes: where its operands are, and its scales.
@@ -285,14 +282,14 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
         int tm, tn;
         if constexpr (!SPLIT) {
             place(tile, ntiles, tiles_m, tiles_n, tm, tn);
-            steps = max(KB, S);
+            steps = max((K + BK - 1) / BK, S);
         } else {       // (neighbours of different parts, so that with eight parts an XCD has one part of K of both operands)
             const int at = tile / parts;
             part = tile - at * parts;
             tn = at / tiles_m;
             tm = at - tn * tiles_m;
-            k_first = part * split_steps * 128;
-            steps = max(min(split_steps, KB - part * split_steps), S);
+            k_first = part * split_blocks * 128;
+            steps = max((min(split_blocks * 128, K - k_first) + BK - 1) / BK, S);
         }
         if constexpr (GROUPED) r = find_tile(g, expert_tiles(g, 0, C::BM), tm, C::BM);
         else r = Rows{0, tm * C::BM, min((tm + 1) * C::BM, (int)g.rows)};
@@ -307,13 +304,13 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
         };
 #pragma unroll
         for (int i = 0; i < C::XL; ++i) {
-            const int m = (i * NW + wave) * 8 + lane / 8;
-            xo[i] = x_offset(m, K) + (uint32_t)((lane & 7) ^ x_key(m)) * 16;
+            const int m = (i * NW + wave) * C::EACH + lane / (BK / 16);
+            xo[i] = x_offset(m, K) + (uint32_t)((lane % (BK / 16)) ^ C::x_key(m)) * 16;
         }
 #pragma unroll
         for (int i = 0; i < C::WL; ++i) {
-            const int n = (i * NW + wave) * 8 + lane / 8;
-            wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane & 7) ^ w_key_of<TN>(n)) * 16;
+            const int n = (i * NW + wave) * C::EACH + lane / (BK / 16);
+            wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane % (BK / 16)) ^ C::w_key(n)) * 16;
         }
         side ^= 1;
         if constexpr (!SPLIT) {
@@ -330,11 +327,11 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
 
     // ---- fragments: row l % 16 of X; for the i-th of W, of the wave's columns that which leaves a lane 4 TN consecutive ones of the output
     const int l16 = lane & 15, xr = wm * TM * 16 + l16, wr = wn * 16 * TN + l16 / 4 * 4 * TN + l16 % 4;
-    const int xf_at = xr * 128 + ((lane >> 4) ^ x_key(xr)) * 16;
-    const int wf_at = C::BM * 128 + wr * 128 + ((lane >> 4) ^ w_key_of<TN>(wr)) * 16;    // (rows 4 i on have the same key)
-    auto read = [&](int at, int more, v4i (&f)[2]) {
+    const int xf_at = xr * BK + ((lane >> 4) ^ C::x_key(xr)) * 16;
+    const int wf_at = C::BM * BK + wr * BK + ((lane >> 4) ^ C::w_key(wr)) * 16;    // (rows 4 i on have the same key)
+    auto read = [&](int at, int more, v4i (&f)[H]) {
         f[0] = *reinterpret_cast<const v4i*>(smem + at + more);
-        f[1] = *reinterpret_cast<const v4i*>(smem + (at ^ 64) + more);
+        if constexpr (H > 1) f[1] = *reinterpret_cast<const v4i*>(smem + (at ^ 64) + more);
     };
 
     begin_tile();
@@ -348,14 +345,14 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
     block_barrier();
 
     constexpr int RING = TM < 4 ? TM : 4, AHEAD = RING / 2 ? RING / 2 : 1;               // X fragments are read so many of them ahead
-    constexpr int GROUPS = TM < 4 ? TM - 1 : EARLY_GROUPS, SPOTS = 2 * TN * GROUPS, EVERY = SPOTS / LPS ? SPOTS / LPS : 1, AT_ONCE = (LPS * EVERY + SPOTS - 1) / SPOTS;   // a step's loads go out among the products of so many X fragments
-    v4i xf[RING][2], wf[TN][2];
+    constexpr int GROUPS = TM < 4 ? TM - 1 : TM - 1 < 6 / H ? TM - 1 : 6 / H, SPOTS = H * TN * GROUPS, EVERY = SPOTS / LPS ? SPOTS / LPS : 1, AT_ONCE = (LPS * EVERY + SPOTS - 1) / SPOTS;   // a step's loads go out among the products of so many X fragments
+    v4i xf[RING][H], wf[TN][H];
     int stage = 0;             // of this step, as a place in LDS
     auto after = [](int at) { return at == (S - 1) * C::STAGE ? 0 : at + C::STAGE; };
 #pragma unroll
-    for (int i = 0; i < TN; ++i) read(wf_at, i * 512, wf[i]);
+    for (int i = 0; i < TN; ++i) read(wf_at, i * 4 * BK, wf[i]);
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) read(xf_at, j * 2048, xf[j]);
+    for (int j = 0; j < AHEAD; ++j) read(xf_at, j * 16 * BK, xf[j]);
 
     for (;;) {
         const Rows here = r;       // (the loads move on to the next tile before this one is done)
@@ -366,14 +363,14 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
 #pragma unroll
             for (int i = 0; i < TN; ++i) acc[j][i] = v4i{0, 0, 0, 0};
         auto step = [&]() {
-            const int next = after(stage), fill = S == 2 ? next : stage == 0 ? (S - 1) * C::STAGE : stage - C::STAGE;
+            const int next = after(stage), fill = stage == 0 ? (S - 1) * C::STAGE : stage - C::STAGE;
             auto meet = [&]() {
                 wait_vmcnt<(EARLY ? S - 3 : S - 2) * LPS>();
                 if constexpr (!EARLY) wait_lgkmcnt0();    // (early: what was read of the stage before has been multiplied)
                 block_barrier();
             };
             if constexpr (EARLY) meet();
-            auto fetch = [&](int q) { read(xf_at + (q < TM ? stage : next), q % TM * 2048, xf[q % RING]); };     // X fragment q from the front of this stage
+            auto fetch = [&](int q) { read(xf_at + (q < TM ? stage : next), q % TM * 16 * BK, xf[q % RING]); };     // X fragment q from the front of this stage
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
                 if (EARLY || j + AHEAD < TM) fetch(j + AHEAD);
@@ -384,12 +381,12 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
                     for (int q = 0; q < AHEAD; ++q) fetch(TM + q);
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < H; ++h)
 #pragma unroll
                     for (int i = 0; i < TN; ++i) {
                         acc[j][i] = mfma(wf[i][h], xf[j % RING][h], acc[j][i]);
-                        if (j == TM - 1 && h == 1) read(wf_at + next, i * 512, wf[i]);
-                        const int spot = (j * 2 + h) * TN + i;
+                        if (j == TM - 1 && h == H - 1) read(wf_at + next, i * 4 * BK, wf[i]);
+                        const int spot = (j * H + h) * TN + i;
 #pragma unroll
                         for (int l = 0; l < AT_ONCE; ++l)
                             if (spot < SPOTS && spot % EVERY == 0 && spot / EVERY * AT_ONCE + l < LPS) issue(fill, spot / EVERY * AT_ONCE + l);
@@ -461,7 +458,7 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
                     const v4i y = *reinterpret_cast<const v4i*>(from);
                     // (rows of an odd number of columns begin at any element)
                     if (inside || (row0 + at < here.end && have >= EACH)) {
-                        __builtin_memcpy(out, &y, 16);
+                        __builtin_nontemporal_store(y, reinterpret_cast<v4i_any*>(out));
                     } else if (row0 + at < here.end) {
                         const Out* const piece = reinterpret_cast<const Out*>(from);
 #pragma clang loop unroll(disable) vectorize(disable)
@@ -479,14 +476,14 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
 }
 
 template <bool GROUPED, int OUT, typename C>
-hipError_t launch_tile(const Int8Args& g, int parts, int part_steps, hipStream_t st)
+hipError_t launch_tile(const Int8Args& g, int parts, int part_blocks, hipStream_t st)
 {
     static LdsAttrOnce attr;
     const hipError_t e = attr.ensure(reinterpret_cast<const void*>(int8_tile_kernel<GROUPED, OUT, C>), C::lds());
     if (e != hipSuccess) return e;
     const int64_t tiles_m = GROUPED ? g.rows / C::BM + std::min<int64_t>(g.experts, g.rows) : (g.rows + C::BM - 1) / C::BM, tiles_n = (g.N + C::BN - 1) / C::BN;
     const int64_t grid = std::min<int64_t>(tiles_m * tiles_n * parts, (int64_t)compute_units() * (163840 / C::lds()));
-    hipLaunchKernelGGL((int8_tile_kernel<GROUPED, OUT, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(), st, g, (int)tiles_m, (int)tiles_n, parts, part_steps);
+    hipLaunchKernelGGL((int8_tile_kernel<GROUPED, OUT, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(), st, g, (int)tiles_m, (int)tiles_n, parts, part_blocks);
     return hipGetLastError();
 }
 
@@ -522,11 +519,11 @@ __global__ __launch_bounds__(256) void int8_join_kernel(Int8Args g, const int* p
 
 // A product in parts of K on tiles of C, and their sum.
 template <int OUT, typename C>
-hipError_t launch_parts(Int8Args g, int parts, int part_steps, void* partial, hipStream_t st)
+hipError_t launch_parts(Int8Args g, int parts, int part_blocks, void* partial, hipStream_t st)
 {
     Int8Args sums = g;
     sums.out = partial;
-    const hipError_t e = launch_tile<false, kSums, C>(sums, parts, part_steps, st);
+    const hipError_t e = launch_tile<false, kSums, C>(sums, parts, part_blocks, st);
     if (e != hipSuccess) return e;
     const int64_t total = g.rows * ((g.N + 3) / 4);
     hipLaunchKernelGGL(int8_join_kernel<OUT>, dim3((unsigned)std::min<int64_t>((total + 255) / 256, 1 << 20)), dim3(256), 0, st, g, static_cast<const int*>(partial), parts);
@@ -548,7 +545,7 @@ hipError_t launch_stream(const Int8Args& g, hipStream_t st)
 // How a product runs.
 struct Plan {
     int kind = 0;              // 0 .. 4: few rows (rows and columns of a tile below), 5 ..: tiles
-    int parts = 1, part_steps = 0;
+    int parts = 1, part_blocks = 0;
 };
 
 constexpr int kKinds = 9, kFew = 5;
@@ -564,7 +561,7 @@ Plan plan_int8(const Int8Args& g, bool grouped, size_t room)
         const int64_t KB = (g.K + 127) / 128;
         auto each = [&]() { return std::max<int64_t>((KB + p.parts - 1) / p.parts, 4); };
         while (p.parts > 1 && ((size_t)p.parts * g.rows * g.N * 4 > room || (p.parts - 1) * each() >= KB)) p.parts >>= 1;
-        p.part_steps = (int)each();
+        p.part_blocks = (int)each();
         return p;
     }
     p.kind = g.rows <= 16 ? 0 : g.rows <= 32 ? 2 : g.rows <= 128 ? 5 : g.rows <= 1024 ? 6 : 7;
@@ -574,15 +571,21 @@ Plan plan_int8(const Int8Args& g, bool grouped, size_t room)
 template <bool GROUPED, int OUT>
 hipError_t launch(const Int8Args& g, const Plan& p, void* partial, hipStream_t st)
 {
-    typedef Tile<2, 4, 2, 2, 4> Tile64;            // 64 x 128
-    typedef Tile<4, 4, 2, 2, 4> Tile128;           // 128 x 128
-    typedef Tile<8, 4, 2, 4, 2> Tile256;           // 256 x 256
-    typedef Tile<8, 8, 2, 2, 2> Tile256b;
+#ifndef T64
+#define T64 2, 4, 2, 2, 128, 4, true
+#define T128 4, 4, 2, 2, 128, 4, true
+#define T256 8, 4, 2, 4, 128, 2
+#define T256B 8, 8, 2, 2, 128, 2
+#endif
+    typedef Tile<T64> Tile64;            // 64 x 128
+    typedef Tile<T128> Tile128;           // 128 x 128
+    typedef Tile<T256> Tile256;           // 256 x 256
+    typedef Tile<T256B> Tile256b;
     if constexpr (!GROUPED) {
         if (p.parts > 1) {
-            if (p.kind == 5) return launch_parts<OUT, Tile64>(g, p.parts, p.part_steps, partial, st);
-            if (p.kind == 6) return launch_parts<OUT, Tile128>(g, p.parts, p.part_steps, partial, st);
-            return launch_parts<OUT, Tile256>(g, p.parts, p.part_steps, partial, st);
+            if (p.kind == 5) return launch_parts<OUT, Tile64>(g, p.parts, p.part_blocks, partial, st);
+            if (p.kind == 6) return launch_parts<OUT, Tile128>(g, p.parts, p.part_blocks, partial, st);
+            return launch_parts<OUT, Tile256>(g, p.parts, p.part_blocks, partial, st);
         }
     }
     switch (p.kind) {

@@ -197,7 +197,7 @@ hipError_t launch_int8_grouped_gemm(const void* a, const float* a_scales, int64_
                                     const int32_t* index, int64_t rows, int64_t experts, int64_t N, int64_t K, void* out, bool out_f32, hipStream_t st);
 
 // a router's choices and the rows by expert; counts: moe_count_bytes bytes of scratch
-size_t moe_count_bytes(int64_t tokens, int64_t experts);
+size_t moe_count_bytes(int64_t tokens, int64_t experts, int64_t top);
 hipError_t launch_moe_route(const void* logits, int64_t stride, bool f32, const float* bias, int64_t tokens, int64_t experts, int64_t top, int64_t groups, int64_t top_groups, float scale,
                             bool sigmoid, bool renorm, bool sum2, float* weights, int32_t* chosen, int32_t* offsets, int32_t* rows, int32_t* places, void* counts, hipStream_t st);
 hipError_t launch_moe_combine(const void* y, int64_t y_rows, bool y_f32, const int32_t* places, const float* weights, const void* shared, bool shared_f32, int64_t tokens, int64_t top,

@@ -19,7 +19,7 @@ fp4mr_status_t status(hipError_t e) { return e == hipSuccess ? FP4MR_OK : FP4MR_
 
 extern "C" {
 
-size_t moe_workspace_bytes(int64_t T, int64_t experts, int64_t top) { return routed(T, experts, top) ? moe_count_bytes(T, experts) : 0; }
+size_t moe_workspace_bytes(int64_t T, int64_t experts, int64_t top) { return routed(T, experts, top) ? moe_count_bytes(T, experts, top) : 0; }
 
 fp4mr_status_t moe_route(const void* logits, int64_t logits_stride, const float* bias, int64_t T, int64_t experts, int64_t top, int64_t groups, int64_t top_groups, float scale,
                          float* weights_out, int32_t* experts_out, int32_t* rows_out, int32_t* offsets_out, int32_t* places_out, void* workspace, size_t workspace_bytes, uint32_t flags,
@@ -35,7 +35,7 @@ fp4mr_status_t moe_route(const void* logits, int64_t logits_stride, const float*
     if (!aligned(logits, f32 ? 4 : 2) || !aligned(bias, 4) || !aligned(weights_out, 4) || !aligned(experts_out, 4) || !aligned(rows_out, 4) || !aligned(offsets_out, 4) ||
         !aligned(places_out, 4) || !aligned(workspace, 16))
         return FP4MR_ERR_ALIGN;
-    const size_t need = moe_count_bytes(T, experts);
+    const size_t need = moe_count_bytes(T, experts, top);
     if (need && (!workspace || workspace_bytes < need)) return FP4MR_ERR_WORKSPACE;
     return status(launch_moe_route(logits, logits_stride, f32, bias, T, experts, top, groups, top_groups, scale, (flags & FP4MR_ROUTE_SIGMOID) != 0, (flags & FP4MR_ROUTE_RENORM) != 0,
                                    (flags & FP4MR_ROUTE_GROUP_SUM2) != 0, weights_out, experts_out, offsets_out, rows_out, places_out, workspace, static_cast<hipStream_t>(stream)));

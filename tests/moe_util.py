@@ -30,7 +30,7 @@ def choose(z, top, bias=None, groups=1, top_groups=1, scale=1.0, sigmoid=False, 
         order = [e for e in np.argsort(-c, kind="stable")[:top] if c[e] > -np.inf]
         experts[t, : len(order)] = order
         w = s[order]
-        weights[t, : len(order)] = w * scale / (max(w.sum(), 2.0 ** -100) if renorm else 1.0)
+        weights[t, : len(order)] = w * scale / (max(w.sum(), 2.0 ** -60) if renorm else 1.0)
     flat = experts.reshape(-1)
     order = [f for f in np.argsort(flat, kind="stable") if flat[f] >= 0]
     places = np.full(T * top, -1)

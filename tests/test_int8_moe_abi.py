@@ -81,7 +81,7 @@ def test_router(b):
     for n in ("z", "w", "e", "rows", "off", "places"):
         assert route(**{n: None}) == NULL and route(**{n: fake + 1}) == ALIGN, n
     assert route(bias=fake + 2) == ALIGN and route(z=fake + 2, flags=b.INPUT_F32) == ALIGN and route(ws=fake + 4) == ALIGN
-    assert route(ws=None) == WORKSPACE and route(wsz=b.moe_workspace_bytes(4, 64, 4) - 1) == WORKSPACE
+    assert route(T=100, ws=None) == WORKSPACE and route(T=100, wsz=b.moe_workspace_bytes(100, 64, 4) - 1) == WORKSPACE
     assert route(stride=63) == SHAPE and route(T=-1) == SHAPE and route(T=(1 << 24) + 1) == SHAPE and route(E=0) == SHAPE and route(E=1040, stride=2000) == SHAPE
     assert route(top=0) == SHAPE and route(top=17) == SHAPE and route(top=65, groups=1, top_groups=1) == SHAPE and route(groups=0) == SHAPE and route(groups=7) == SHAPE
     assert route(E=1000, stride=1000, groups=125) == SHAPE and route(top_groups=9) == SHAPE and route(top_groups=0) == SHAPE and route(T=1 << 24, top=65) == SHAPE
@@ -114,7 +114,7 @@ def test_workspaces_are_device_memory_of_their_own_size(b, monkeypatch):
     room = lambda n: torch.empty(n, dtype=torch.uint8)
     bad = (room(1 << 20), room(1).expand(1 << 20).as_subclass(OnDevice), room(1 << 20).as_subclass(OnDevice)[::2])
     for name, run in (("int8_gemm", lambda w: b.int8_gemm(on(64, 4096, dtype=torch.int8), on(64), on(256, 4096, dtype=torch.int8), on(256), workspace=w)),
-                      ("moe_route", lambda w: b.moe_route(on(64, 32), 2, workspace=w))):
+                      ("moe_route", lambda w: b.moe_route(on(100, 32), 2, workspace=w))):
         monkeypatch.setattr(b.lib, name, lambda *a: calls.append(a) or 0)
         for w in bad:
             with pytest.raises(AssertionError):
