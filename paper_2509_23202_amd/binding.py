@@ -121,6 +121,8 @@ try:
                                                      lib.fp4_fused_linear, lib.fp4_w4a16_linear, lib.fp4_workspace_bytes, lib.fp4_packed_bytes)), Fp4mrError)
     _calls.bind8(*(ctypes.cast(f, _p).value for f in (lib.fp8_rmsnorm_quantize, lib.fp8_quantize, lib.fp8_quantize_weights, lib.fp8_gemm, lib.fp8_workspace_bytes,
                                                        lib.fp8_grouped_gemm)))
+    _calls.bind8i(*(ctypes.cast(f, _p).value for f in (lib.int8_rmsnorm_quantize, lib.int8_quantize, lib.int8_gemm, lib.int8_workspace_bytes, lib.int8_grouped_gemm, lib.moe_route,
+                                                        lib.moe_workspace_bytes, lib.moe_combine)))
 except ImportError:
     _calls = None
 
@@ -529,6 +531,10 @@ def int8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residu
     """codes, scales, h = Q(v) with v = h * weight / sqrt(mean(h^2) + eps) and h = bf16(x + residual), or x (then the third result is None).
     x: bf16 [M,K], rows may be apart (K % 16 == 0, K <= 65536); weight: bf16 [K]; residual: bf16 [M,K].  residual_out: where h goes (may be residual
     or x themselves, a new tensor if None); norm_out: bf16 [M,K] to receive v too."""
+    if _calls is not None and residual_out is None and codes is None and scales is None:
+        out = _calls.rmsnorm_quantize8i(x, weight, eps, residual, norm_out)
+        if out is not None:
+            return out
     M, K, stride = _rows(x)
     assert x.device.index == _current_device()
     _is_tensor(weight, torch.bfloat16, K)
@@ -548,6 +554,10 @@ def int8_rmsnorm_quantize(x, weight, eps: float = 1e-6, *, residual=None, residu
 def int8_quantize(x, *, flags: int = 0, codes=None, scales=None):
     """codes, scales = Q(x), a scale per row, of bf16 activations [M,K] (rows may be apart), or with SILU_MUL of silu(x[:, :K]) * x[:, K:] of x [M, 2K]; of weights [N,K], or of
     experts [E,N,K] (contiguous).  K % 16 == 0."""
+    if _calls is not None and codes is None and scales is None:
+        out = _calls.quantize8i(x, flags)
+        if out is not None:
+            return out
     if x.dim() == 3:
         assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous()
         M, K, stride = x.shape[0] * x.shape[1], x.shape[2], x.shape[2]
@@ -578,6 +588,10 @@ def _product8i_out(a_codes, a_scales, w_codes, w_scales, dim: int, rows: int, fl
 
 def int8_gemm(a_codes, a_scales, w_codes, w_scales, *, flags: int = 0, out=None, workspace=None):
     """out[M,N] = A W^T (bf16, or fp32 with OUT_F32) from the int8 codes and row scales of activations [M,K] and weights [N,K]; the sums are exact."""
+    if _calls is not None and out is None and workspace is None:
+        got = _calls.gemm8i(a_codes, a_scales, w_codes, w_scales, flags)
+        if got is not None:
+            return got
     M = a_codes.shape[0]
     out, N, K = _product8i_out(a_codes, a_scales, w_codes, w_scales, 2, M, flags, out)
     need = int8_workspace_bytes(M, N, K)
@@ -597,6 +611,10 @@ def int8_grouped_gemm(a_codes, a_scales, w_codes, w_scales, offsets, *, rows=Non
     """Rows offsets[e] .. offsets[e+1] - 1 of out = those rows of A times the weights of expert e, w_codes [E,N,K]; offsets: int32 [E+1].
     rows: int32 [T], the row of A for each row of out (outside A: a row of zeros); without it out has A's rows.  Rows of out that no expert has are
     not written (a new out holds what its memory held)."""
+    if _calls is not None and out is None:
+        got = _calls.gemm8i(a_codes, a_scales, w_codes, w_scales, flags, offsets, rows)
+        if got is not None:
+            return got
     _is_tensor(offsets, torch.int32, w_codes.shape[0] + 1)
     T = a_codes.shape[0]
     if rows is not None:
@@ -619,6 +637,10 @@ def moe_route(logits, top: int, *, bias=None, groups: int = 1, top_groups: int =
     (int32 [E+1]), and each choice's row (int32 [T,top]).  flags: ROUTE_SIGMOID (scores; else softmax), ROUTE_RENORM (weights divided by their sum), ROUTE_GROUP_SUM2.  bias: float32 [E],
     added to the scores for the choice alone.  groups, top_groups: only the experts of the best groups may be chosen.  An expert of -inf is not chosen; a choice that a token does
     not have is -1, with a weight of 0 and a place of -1, and has no row (rows behind offsets[E] are not written)."""
+    if _calls is not None and workspace is None:
+        got = _calls.route(logits, top, bias, groups, top_groups, scale, flags)
+        if got is not None:
+            return got
     assert logits.is_cuda and logits.device.index == _current_device() and logits.dim() == 2 and logits.dtype in (torch.bfloat16, torch.float32)
     T, E = logits.shape
     assert logits.stride(1) == 1 or E <= 1
@@ -643,6 +665,10 @@ def moe_route(logits, top: int, *, bias=None, groups: int = 1, top_groups: int =
 def moe_combine(y, places, weights, *, shared=None, flags: int = 0, out=None):
     """out[T,H] = shared + sum over j of weights[:, j] * y[places[:, j]], in float32 and rounded once (bf16, or float32 with OUT_F32).  y: bf16 or float32 [rows,H]; places: int32 [T,top]
     (outside y: the weight times zero); weights: float32 [T,top]; shared: bf16 or float32 [T,H] (may be out)."""
+    if _calls is not None and out is None:
+        got = _calls.combine(y, places, weights, shared, flags)
+        if got is not None:
+            return got
     assert y.dim() == 2 and places.dim() == 2 and y.dtype in (torch.bfloat16, torch.float32)
     R, H = y.shape
     T, top = places.shape

@@ -44,6 +44,16 @@ struct Entry8 {     // of the 8-bit linear layers
     decltype(&fp8_workspace_bytes) workspace_bytes8;
     decltype(&fp8_grouped_gemm) grouped_gemm8;
 } entry8;
+struct Entry8i {    // of the 8-bit integer layers, and of the router
+    decltype(&int8_rmsnorm_quantize) rmsnorm_quantize8i;
+    decltype(&int8_quantize) quantize8i;
+    decltype(&int8_gemm) gemm8i;
+    decltype(&int8_workspace_bytes) workspace_bytes8i;
+    decltype(&int8_grouped_gemm) grouped_gemm8i;
+    decltype(&moe_route) route;
+    decltype(&moe_workspace_bytes) route_workspace_bytes;
+    decltype(&moe_combine) combine;
+} entry8i;
 PyObject* error;   // the binding's exception, called with a status
 
 // an argument that is a plain Python int in range
@@ -322,6 +332,170 @@ PyObject* gemm8(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the integer form of the 8-bit layers, and the router: on the current device
+bool here(const at::Tensor* t) { return !t || t->get_device() == c10::hip::current_device(); }
+bool codes8i(const at::Tensor& codes, const at::Tensor& scales, int64_t dim)      // [.., rows, K] and [.., rows]
+{
+    if (codes.scalar_type() != at::kChar || scales.scalar_type() != at::kFloat || codes.dim() != dim || scales.dim() != dim - 1 || !codes.is_contiguous() || !scales.is_contiguous()) return false;
+    return codes.size(dim - 2) == scales.size(dim - 2) && (dim == 2 || codes.size(0) == scales.size(0)) && here(&codes) && here(&scales);
+}
+
+// rmsnorm_quantize8i(x, weight, eps, residual, norm_out): into new tensors, but for norm_out
+PyObject* rmsnorm_quantize8i(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight, *residual, *norm;
+    if (n != 5 || !plain() || !tensor(args[0], x) || !tensor(args[1], weight) || !PyFloat_CheckExact(args[2]) || !tensor(args[3], residual, true) || !tensor(args[4], norm, true) ||
+        !bf16_strided(*x))
+        Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1);
+    if (M <= 0 || K <= 0 || weight->scalar_type() != at::kBFloat16 || weight->dim() != 1 || weight->size(0) != K || !weight->is_contiguous() || !bf16_like(residual, M, K) ||
+        !bf16_like(norm, M, K) || !here(x) || !here(weight) || !here(residual) || !here(norm))
+        Py_RETURN_NONE;
+    const at::Tensor codes = empty({M, K}, at::kChar, *x), scales = empty({M}, at::kFloat, *x);
+    at::Tensor sum;
+    if (residual) sum = empty({M, K}, at::kBFloat16, *x);
+    const float eps = (float)PyFloat_AS_DOUBLE(args[2]);
+    const void *const px = x->data_ptr(), *const pw = weight->data_ptr();
+    void *const pr = pointer(residual), *const pn = pointer(norm), *const pc = codes.data_ptr(), *const ps = residual ? sum.data_ptr() : nullptr, *const st = stream();
+    float* const psc = static_cast<float*>(scales.data_ptr());
+    const int64_t apart = row_stride(*x);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8i.rmsnorm_quantize8i(px, apart, pr, pw, M, K, eps, pc, psc, ps, pn, 0, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({codes, scales, sum});
+    END_HANDLE_TH_ERRORS
+}
+
+// quantize8i(x, flags): rows, or contiguous weights of several experts
+PyObject* quantize8i(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor* x;
+    int64_t flags;
+    if (n != 2 || !plain() || !tensor(args[0], x) || !integer(args[1], flags) || (flags & ~(int64_t)FP4MR_SILU_MUL) || x->scalar_type() != at::kBFloat16 || !here(x) ||
+        !(x->dim() == 2 ? x->stride(1) == 1 : x->dim() == 3 && x->is_contiguous()))
+        Py_RETURN_NONE;
+    const int64_t held = x->size(-1), K = flags ? held / 2 : held, outer = x->dim() == 3 ? x->size(0) : 1, inner = x->size(-2), M = outer * inner;
+    if (M <= 0 || K <= 0 || (flags && held % 2 != 0)) Py_RETURN_NONE;
+    const at::Tensor codes = x->dim() == 3 ? empty({outer, inner, K}, at::kChar, *x) : empty({M, K}, at::kChar, *x);
+    const at::Tensor scales = x->dim() == 3 ? empty({outer, inner}, at::kFloat, *x) : empty({M}, at::kFloat, *x);
+    const void* const px = x->data_ptr();
+    void *const pc = codes.data_ptr(), *const st = stream();
+    float* const psc = static_cast<float*>(scales.data_ptr());
+    const int64_t apart = x->dim() == 3 ? held : row_stride(*x);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8i.quantize8i(px, apart, M, K, pc, psc, (uint32_t)flags, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({codes, scales});
+    END_HANDLE_TH_ERRORS
+}
+
+// gemm8i(a_codes, a_scales, w_codes, w_scales, flags), and with two arguments more, offsets and rows (or None), the product by expert
+PyObject* gemm8i(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *a, *sa, *w, *sw, *offsets = nullptr, *rows = nullptr;
+    int64_t flags;
+    const bool grouped = n == 7;
+    if ((n != 5 && !grouped) || !plain() || !tensor(args[0], a) || !tensor(args[1], sa) || !tensor(args[2], w) || !tensor(args[3], sw) || !integer(args[4], flags) ||
+        (flags & ~(int64_t)FP4MR_OUT_F32) || !codes8i(*a, *sa, 2) || !codes8i(*w, *sw, grouped ? 3 : 2) || a->size(1) != w->size(-1))
+        Py_RETURN_NONE;
+    if (grouped && (!tensor(args[5], offsets) || !tensor(args[6], rows, true) || offsets->scalar_type() != at::kInt || offsets->dim() != 1 || !offsets->is_contiguous() ||
+                    offsets->numel() != w->size(0) + 1 || !here(offsets) || (rows && (rows->scalar_type() != at::kInt || rows->dim() != 1 || !rows->is_contiguous() || !here(rows)))))
+        Py_RETURN_NONE;
+    const int64_t a_rows = a->size(0), M = rows ? rows->size(0) : a_rows, N = w->size(-2), K = w->size(-1);
+    if (M <= 0 || N <= 0 || K <= 0) Py_RETURN_NONE;
+    const at::Tensor out = empty({M, N}, flags ? at::kFloat : at::kBFloat16, *a);
+    at::Tensor workspace;
+    const size_t need = grouped ? 0 : entry8i.workspace_bytes8i(M, N, K);
+    if (need) workspace = empty({(int64_t)need}, at::kByte, *a);
+    const void *const pa = a->data_ptr(), *const pw = w->data_ptr();
+    const float *const psa = static_cast<const float*>(sa->data_ptr()), *const psw = static_cast<const float*>(sw->data_ptr());
+    const int32_t *const po = static_cast<const int32_t*>(pointer(offsets)), *const pr = static_cast<const int32_t*>(pointer(rows));
+    void *const to = out.data_ptr(), *const pws = need ? workspace.data_ptr() : nullptr, *const st = stream();
+    const int64_t experts = grouped ? w->size(0) : 1;
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    if (grouped) status = entry8i.grouped_gemm8i(pa, psa, a_rows, pw, psw, po, pr, M, experts, N, K, to, (uint32_t)flags, st);
+    else status = entry8i.gemm8i(pa, psa, pw, psw, M, N, K, to, pws, need, (uint32_t)flags, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// route(logits, top, bias, groups, top_groups, scale, flags)
+PyObject* route(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *z, *bias;
+    int64_t top, groups, top_groups, flags;
+    if (n != 7 || !plain() || !tensor(args[0], z) || !integer(args[1], top) || !tensor(args[2], bias, true) || !integer(args[3], groups) || !integer(args[4], top_groups) ||
+        !PyFloat_CheckExact(args[5]) || !integer(args[6], flags) || flags < 0 || flags > 0xffffffffll || z->dim() != 2 || !here(z) || !here(bias))
+        Py_RETURN_NONE;
+    const int64_t T = z->size(0), E = z->size(1);
+    const bool f32 = z->scalar_type() == at::kFloat;
+    if ((!f32 && z->scalar_type() != at::kBFloat16) || T <= 0 || E <= 0 || z->stride(1) != 1 || top <= 0 || top > E || T > (1ll << 24) ||
+        (bias && (bias->scalar_type() != at::kFloat || bias->dim() != 1 || bias->size(0) != E || !bias->is_contiguous())))
+        Py_RETURN_NONE;
+    const at::Tensor weights = empty({T, top}, at::kFloat, *z), experts = empty({T, top}, at::kInt, *z), rows = empty({T * top}, at::kInt, *z), offsets = empty({E + 1}, at::kInt, *z),
+                     places = empty({T, top}, at::kInt, *z);
+    at::Tensor workspace;
+    const size_t need = entry8i.route_workspace_bytes(T, E, top);
+    if (need) workspace = empty({(int64_t)need}, at::kByte, *z);
+    const void* const pz = z->data_ptr();
+    const float* const pb = static_cast<const float*>(pointer(bias));
+    float* const pw = static_cast<float*>(weights.data_ptr());
+    int32_t *const pe = static_cast<int32_t*>(experts.data_ptr()), *const pr = static_cast<int32_t*>(rows.data_ptr()), *const po = static_cast<int32_t*>(offsets.data_ptr()),
+            *const pp = static_cast<int32_t*>(places.data_ptr());
+    void *const ws = need ? workspace.data_ptr() : nullptr, *const st = stream();
+    const int64_t apart = T > 1 ? z->stride(0) : E;
+    const float scale = (float)PyFloat_AS_DOUBLE(args[5]);
+    const uint32_t all = (uint32_t)flags | (f32 ? FP4MR_INPUT_F32 : 0u);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8i.route(pz, apart, pb, T, E, top, groups, top_groups, scale, pw, pe, pr, po, pp, ws, need, all, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return tuple({weights, experts, rows, offsets, places});
+    END_HANDLE_TH_ERRORS
+}
+
+// combine(y, places, weights, shared, flags)
+PyObject* combine(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *y, *places, *weights, *shared;
+    int64_t flags;
+    if (n != 5 || !plain() || !tensor(args[0], y) || !tensor(args[1], places) || !tensor(args[2], weights) || !tensor(args[3], shared, true) || !integer(args[4], flags) ||
+        (flags & ~(int64_t)FP4MR_OUT_F32) || y->dim() != 2 || places->dim() != 2 || !y->is_contiguous() || !places->is_contiguous() || !weights->is_contiguous() ||
+        places->scalar_type() != at::kInt || weights->scalar_type() != at::kFloat || weights->sizes() != places->sizes() || !here(y) || !here(places) || !here(weights) || !here(shared))
+        Py_RETURN_NONE;
+    const int64_t rows = y->size(0), H = y->size(1), T = places->size(0), top = places->size(1);
+    const bool y_f32 = y->scalar_type() == at::kFloat, s_f32 = shared && shared->scalar_type() == at::kFloat;
+    if ((!y_f32 && y->scalar_type() != at::kBFloat16) || T <= 0 || H <= 0 ||
+        (shared && ((!s_f32 && shared->scalar_type() != at::kBFloat16) || shared->dim() != 2 || shared->size(0) != T || shared->size(1) != H || !shared->is_contiguous())))
+        Py_RETURN_NONE;
+    const at::Tensor out = empty({T, H}, flags ? at::kFloat : at::kBFloat16, *y);
+    const void *const py = y->data_ptr(), *const psh = pointer(shared);
+    const int32_t* const pp = static_cast<const int32_t*>(places->data_ptr());
+    const float* const pw = static_cast<const float*>(weights->data_ptr());
+    void *const to = out.data_ptr(), *const st = stream();
+    const uint32_t all = (uint32_t)flags | (y_f32 ? FP4MR_INPUT_F32 : 0u) | (s_f32 ? FP4MR_SHARED_F32 : 0u);
+    fp4mr_status_t status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = entry8i.combine(py, rows, pp, pw, psh, T, top, H, to, all, st);
+    Py_END_ALLOW_THREADS;
+    if (status != FP4MR_OK) return refused(status);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
 // The addresses of the entry points of `to` in its order, from Python integers.
 template <typename E>
 bool addresses(PyObject* const* args, E& to)
@@ -365,6 +539,17 @@ PyObject* bind8(PyObject*, PyObject* const* args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// bind8i(addresses of the eight entry points, in the order of Entry8i), behind bind()
+PyObject* bind8i(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != (Py_ssize_t)(sizeof(Entry8i) / sizeof(void*))) {
+        PyErr_SetString(PyExc_TypeError, "bind8i() takes eight addresses");
+        return nullptr;
+    }
+    if (!addresses(args, entry8i)) return nullptr;
+    Py_RETURN_NONE;
+}
+
 template <typename F>
 PyCFunction method(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -377,6 +562,12 @@ PyMethodDef methods[] = {{"bind", method(bind), METH_FASTCALL, nullptr},
                          {"quantize8", method(quantize8), METH_FASTCALL, nullptr},
                          {"quantize_weights8", method(quantize_weights8), METH_FASTCALL, nullptr},
                          {"gemm8", method(gemm8), METH_FASTCALL, nullptr},
+                         {"bind8i", method(bind8i), METH_FASTCALL, nullptr},
+                         {"rmsnorm_quantize8i", method(rmsnorm_quantize8i), METH_FASTCALL, nullptr},
+                         {"quantize8i", method(quantize8i), METH_FASTCALL, nullptr},
+                         {"gemm8i", method(gemm8i), METH_FASTCALL, nullptr},
+                         {"route", method(route), METH_FASTCALL, nullptr},
+                         {"combine", method(combine), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
