@@ -219,40 +219,43 @@ __global__ __launch_bounds__(C::WAVES * 64) void int8_stream_kernel(Int8Args g, 
 }
 
 // ---------------------------------------------------------------- tiles
-// BM x BN to a workgroup of NWM x NWN waves, each 16 TM x 16 TN; a workgroup walks tiles.  A stage is 128 columns of both operands' rows in LDS, eight rows to a 1 KB direct-to-LDS load; the sixteen-byte
-// pieces of a row lie exchanged by a key, so that sixteen rows' reads of one piece touch every bank once.  A step multiplies a stage: the W fragments stay in registers, the X fragments pass through a few
-// buffers.  The requests for the stage S - 1 steps on go out between the products; when this tile's have all gone out, they are the next tile's, whose first stages are there before this tile's output has left.
-//   Two stages: before its last X fragment a wave has read all it needs of the stage.  There it waits for its loads of the next one, the workgroup meets, and the last fragment's products cover the reads of
-// the next step's first fragments.  More stages: a step begins with the meeting.
+// BM x BN to NWM x NWN waves, each 16 TM x 16 TN; a workgroup walks tiles.  A stage is 128 columns of both operands' rows in LDS, eight rows to a 1 KB direct-to-LDS load; the sixteen-byte pieces of a row lie
+// exchanged by a key, so that sixteen rows' reads of one piece touch every bank once.  A step multiplies a stage.  The loads of the stage S - 1 steps on go out in it; when a tile's have all gone out, they are the
+// next tile's, whose first stages are there before this tile's output has left.
+//   FEED waves beside those that multiply do nothing but load.  A wave that issues loads is held up by each (26 bytes a ns to a wave is what goes out, 105 to 145 to a compute unit from eight waves, 88 from four),
+// and one that stores waits for its stores with its loads, which come back in order: so the waves that multiply neither wait for memory nor load, and a tile's output leaves under the next tile's products
+// (128 x 128 with four more waves for the loads: 2048 x 4096 x 14336 130 -> 104 us, 201 x 10240 x 8192 30 -> 27).  A step begins with a meeting, which says that the next stage is there and that the stage before is
+// free.  AHEAD: all fragments of the next step are read while this one's are multiplied, into a second copy of their registers; else the W fragments stay, and the X fragments pass through a few buffers.
+//   Without them (256 x 256, which has no registers for more than eight waves) the waves that multiply load, and there are two stages: before its last X fragment a wave has read all it needs of the stage.  There it
+// waits for its loads of the next one, the workgroup meets, and the last fragment's products cover the reads of the next step's first fragments.
 //   A tile takes S steps at least: the meeting in a step that is not one of its last S - 1 stands between a tile's output, which reads its scales, and the loads of the scales two tiles on.
-template <int TM_, int TN_, int NWM_, int NWN_, int BK_, int STAGES_, bool EARLY_ = false>
+template <int TM_, int TN_, int NWM_, int NWN_, int STAGES_, int FEED_, bool AHEAD_ = false>
 struct Tile {
-    static constexpr int TM = TM_, TN = TN_, NWM = NWM_, NWN = NWN_, BK = BK_, S = STAGES_, NW = NWM * NWN;
-    static constexpr bool EARLY = EARLY_;
-    static constexpr int BM = 16 * TM * NWM, BN = 16 * TN * NWN, EACH = 1024 / BK;     // EACH: rows to a load
-    static constexpr int STAGE = (BM + BN) * BK, SCALES = (BM + BN) * 4;
-    static constexpr int XL = BM / EACH / NW, WL = BN / EACH / NW, LPS = XL + WL;      // loads of a wave for a step: X, W
+    static constexpr int TM = TM_, TN = TN_, NWM = NWM_, NWN = NWN_, S = STAGES_, NW = NWM * NWN, FEED = FEED_, LW = FEED ? FEED : NW;       // LW: waves that load
+    static constexpr bool AHEAD = AHEAD_;
+    static constexpr int BM = 16 * TM * NWM, BN = 16 * TN * NWN;
+    static constexpr int STAGE = (BM + BN) * 128, SCALES = (BM + BN) * 4;
+    static constexpr int XL = BM / 8 / LW, WL = BN / 8 / LW, LPS = XL + WL;   // loads of a wave for a step: X, W
     static constexpr int kScales = S * STAGE;                                 // of two tiles in turn
     static constexpr int kRoom = kScales + 2 * SCALES, ROOM = 512 * TN;       // for the output, of each wave
     static constexpr int lds() { return kRoom + NW * ROOM; }
-    // What the pieces of a row are exchanged by, so that the sixteen rows of a fragment (of W: four in each of four runs of 4 TN) have every pair of key and place within 256 bytes once.
-    static __device__ __forceinline__ int x_key(int row) { return BK == 128 ? row >> 1 & 7 : row >> 2 & 3; }
-    static __device__ __forceinline__ int w_key(int row) { return BK == 128 ? (row >> 1 & 1) | (row / (4 * TN) & 3) << 1 : row / (4 * TN) & 3; }
-    static_assert((BK == 64 || BK == 128) && BM % (EACH * NW) == 0 && BN % (EACH * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && S >= (EARLY ? 3 : 2) && (S - 1) * LPS < 64 && lds() <= 163840, "");
+    static_assert(BM % (8 * LW) == 0 && BN % (8 * LW) == 0 && BM % 64 == 0 && BN % 64 == 0 && (FEED ? S >= 3 : S == 2 && !AHEAD) && (S - 1) * LPS < 64 && lds() <= 163840, "");
 };
+
+// What the pieces of a row of W are exchanged by: a fragment has four rows in each of four runs of 4 TN.
+template <int TN>
+__device__ __forceinline__ int w_key_of(int row) { return (row >> 1 & 1) | (row / (4 * TN) & 3) << 1; }
 
 // split_parts: a unit of work is one part of K of a tile, each of split_blocks times 128 columns but the last, and what leaves (OUT = kSums) is its sums, to the part's own copy of the output.
 template <bool GROUPED, int OUT, typename C>
-__global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int tiles_m, int tiles_n, int split_parts, int split_blocks)
+__global__ __launch_bounds__((C::NW + C::FEED) * 64) void int8_tile_kernel(Int8Args g, int tiles_m, int tiles_n, int split_parts, int split_blocks)
 {
     constexpr bool SPLIT = OUT == kSums;
     static_assert(!SPLIT || !GROUPED, "");
     constexpr int TM = C::TM, TN = C::TN, NW = C::NW, S = C::S, LPS = C::LPS;
-    constexpr int BK = C::BK, H = BK / 64;      // H: MFMAs along a stage
-    constexpr bool EARLY = C::EARLY;
+    constexpr bool FED = C::FEED > 0;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int wm = wave % C::NWM, wn = wave / C::NWM;
     const int K = (int)g.K, parts = SPLIT ? split_parts : 1;
     const bool gather = GROUPED && g.index != nullptr;
     if constexpr (GROUPED) tiles_m = count_tiles(g, expert_tiles(g, 0, C::BM), C::BM, tiles_m);
@@ -260,40 +263,45 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
     int tile = blockIdx.x;
     if (tile >= ntiles) return;
 
-    // ---- the tile whose operands are requested.  Rows that it does not have lie outside of the operand: their loads bring zeros.
+    // ---- a tile: its rows, columns and steps, and for the waves that load where its operands are.  Rows that it does not have lie outside of the operand: their loads bring zeros.
     Rows r{0, 0, 0};
     int n0 = 0, part = 0, side = 0, k_first = 0, steps = 0;
-    __amdgpu_buffer_rsrc_t rx, rw;
-    uint32_t xo[C::XL], wo[C::WL];
-    int t = 0;                 // the step whose loads go out
-    auto issue = [&](int stage, int i) {
-        const int at = k_first + t * BK;
-        if (i < C::XL) {
-            load_lds16(rx, smem, stage + (i * NW + wave) * 1024, xo[i < C::XL ? i : 0], at);
-        } else {
-            const int q = i - C::XL, j = q >= 0 && q < C::WL ? q : 0;
-            const int n = (j * NW + wave) * C::EACH + lane / (BK / 16), piece = (lane % (BK / 16)) ^ C::w_key(n);
-            load_lds16(rw, smem, stage + C::BM * BK + (j * NW + wave) * 1024, wo[j] | (at + piece * 16 < K ? 0u : kOutside), at);
-        }
-    };
-    // In front of a tile's first codes: where its operands are, and its scales.
-    auto begin_tile = [&]() {
-        const int lane = kept_here((int)threadIdx.x & 63);
+    auto locate = [&]() {
         int tm, tn;
         if constexpr (!SPLIT) {
             place(tile, ntiles, tiles_m, tiles_n, tm, tn);
-            steps = max((K + BK - 1) / BK, S);
+            steps = max((K + 127) / 128, S);
         } else {       // (neighbours of different parts, so that with eight parts an XCD has one part of K of both operands)
             const int at = tile / parts;
             part = tile - at * parts;
             tn = at / tiles_m;
             tm = at - tn * tiles_m;
             k_first = part * split_blocks * 128;
-            steps = max((min(split_blocks * 128, K - k_first) + BK - 1) / BK, S);
+            steps = max((min(split_blocks * 128, K - k_first) + 127) / 128, S);     // (a part that is not the last has as many blocks, and what is past K is zeros)
         }
         if constexpr (GROUPED) r = find_tile(g, expert_tiles(g, 0, C::BM), tm, C::BM);
         else r = Rows{0, tm * C::BM, min((tm + 1) * C::BM, (int)g.rows)};
         n0 = tn * C::BN;
+        side ^= 1;
+    };
+    __amdgpu_buffer_rsrc_t rx, rw;
+    uint32_t xo[C::XL], wo[C::WL];
+    int t = 0;                 // the step whose loads go out
+    const int lw = FED ? wave - NW : wave;         // among the waves that load
+    auto issue = [&](int stage, int i) {
+        const int at = k_first + t * 128;
+        if (i < C::XL) {
+            load_lds16(rx, smem, stage + (i * C::LW + lw) * 1024, xo[i < C::XL ? i : 0], at);
+        } else {
+            const int q = i - C::XL, j = q >= 0 && q < C::WL ? q : 0;
+            const int piece = (lane & 7) ^ w_key_of<TN>((j * C::LW + lw) * 8 + lane / 8);
+            load_lds16(rw, smem, stage + C::BM * 128 + (j * C::LW + lw) * 1024, wo[j] | (at + piece * 16 < K ? 0u : kOutside), at);
+        }
+    };
+    // In front of a tile's first codes: its scales too.
+    auto begin_tile = [&]() {
+        const int lane = kept_here((int)threadIdx.x & 63);
+        locate();
         const int64_t x0 = gather ? 0 : r.begin, x_rows = gather ? g.a_rows : r.end - r.begin;
         const int w_rows = min((int)g.N - n0, C::BN);
         rx = make_rsrc(g.a + x0 * K, x_rows * K);
@@ -304,55 +312,91 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
         };
 #pragma unroll
         for (int i = 0; i < C::XL; ++i) {
-            const int m = (i * NW + wave) * C::EACH + lane / (BK / 16);
-            xo[i] = x_offset(m, K) + (uint32_t)((lane % (BK / 16)) ^ C::x_key(m)) * 16;
+            const int m = (i * C::LW + lw) * 8 + lane / 8;
+            xo[i] = x_offset(m, K) + (uint32_t)((lane & 7) ^ x_key(m)) * 16;
         }
 #pragma unroll
         for (int i = 0; i < C::WL; ++i) {
-            const int n = (i * NW + wave) * C::EACH + lane / (BK / 16);
-            wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane % (BK / 16)) ^ C::w_key(n)) * 16;
+            const int n = (i * C::LW + lw) * 8 + lane / 8;
+            wo[i] = (n < w_rows ? (uint32_t)n * (uint32_t)K : kOutside) + (uint32_t)((lane & 7) ^ w_key_of<TN>(n)) * 16;
         }
-        side ^= 1;
         if constexpr (!SPLIT) {
             const __amdgpu_buffer_rsrc_t rs = make_rsrc(g.a_scales + x0, x_rows * 4), rsw = make_rsrc(g.w_scales + (int64_t)r.expert * g.N + n0, (int64_t)w_rows * 4);
 #pragma unroll
-            for (int i = 0; i < (C::BM + C::BN) / 64; i += NW) {
-                const int q = i + wave;
+            for (int i = 0; i < (C::BM + C::BN) / 64; i += C::LW) {
+                const int q = i + lw;
                 if (q < C::BM / 64) load_lds4(rs, smem, C::kScales + side * C::SCALES + q * 256, x_offset(q * 64 + lane, 4));
                 else if (q < (C::BM + C::BN) / 64) load_lds4(rsw, smem, C::kScales + side * C::SCALES + q * 256, (uint32_t)((q - C::BM / 64) * 64 + lane) * 4);
             }
         }
         t = 0;
     };
-
-    // ---- fragments: row l % 16 of X; for the i-th of W, of the wave's columns that which leaves a lane 4 TN consecutive ones of the output
-    const int l16 = lane & 15, xr = wm * TM * 16 + l16, wr = wn * 16 * TN + l16 / 4 * 4 * TN + l16 % 4;
-    const int xf_at = xr * BK + ((lane >> 4) ^ C::x_key(xr)) * 16;
-    const int wf_at = C::BM * BK + wr * BK + ((lane >> 4) ^ C::w_key(wr)) * 16;    // (rows 4 i on have the same key)
-    auto read = [&](int at, int more, v4i (&f)[H]) {
-        f[0] = *reinterpret_cast<const v4i*>(smem + at + more);
-        if constexpr (H > 1) f[1] = *reinterpret_cast<const v4i*>(smem + (at ^ 64) + more);
+    auto move_on = [&]() {     // the loads of this tile have gone out
+        if (tile + (int)gridDim.x < ntiles) {
+            tile += gridDim.x;
+            begin_tile();
+        }
     };
-
-    begin_tile();
+    auto first_stages = [&]() {
+        begin_tile();
 #pragma unroll
-    for (int st = 0; st < S - 1; ++st) {
+        for (int st = 0; st < S - 1; ++st) {
 #pragma unroll
-        for (int i = 0; i < LPS; ++i) issue(st * C::STAGE, i);
-        ++t;
-    }
-    wait_vmcnt<(S - 2) * LPS>();
-    block_barrier();
-
-    constexpr int RING = TM < 4 ? TM : 4, AHEAD = RING / 2 ? RING / 2 : 1;               // X fragments are read so many of them ahead
-    constexpr int GROUPS = TM < 4 ? TM - 1 : TM - 1 < 6 / H ? TM - 1 : 6 / H, SPOTS = H * TN * GROUPS, EVERY = SPOTS / LPS ? SPOTS / LPS : 1, AT_ONCE = (LPS * EVERY + SPOTS - 1) / SPOTS;   // a step's loads go out among the products of so many X fragments
-    v4i xf[RING][H], wf[TN][H];
+            for (int i = 0; i < LPS; ++i) issue(st * C::STAGE, i);
+            ++t;
+        }
+        wait_vmcnt<(S - 2) * LPS>();
+        block_barrier();
+    };
     int stage = 0;             // of this step, as a place in LDS
     auto after = [](int at) { return at == (S - 1) * C::STAGE ? 0 : at + C::STAGE; };
+    auto fill_of = [](int at) { return at == 0 ? (S - 1) * C::STAGE : at - C::STAGE; };     // the stage before this one, for S - 1 steps on
+
+    if constexpr (FED) {
+        if (wave >= NW) {
+            first_stages();
+            for (;;) {
+                const int here_tile = tile, here_steps = steps;
+                for (int half = 0, kt = 0; half < 2; ++half) {
+                    const int to = half ? here_steps : here_steps - S + 1;
+#pragma clang loop unroll(disable)
+                    for (; kt < to; ++kt) {
+                        wait_vmcnt<(S > 3 ? S - 3 : 0) * LPS>();
+                        block_barrier();
+                        const int fill = fill_of(stage);
 #pragma unroll
-    for (int i = 0; i < TN; ++i) read(wf_at, i * 4 * BK, wf[i]);
+                        for (int i = 0; i < LPS; ++i) issue(fill, i);
+                        ++t;
+                        stage = after(stage);
+                    }
+                    if (half == 0) move_on();
+                }
+                if (tile == here_tile) break;
+            }
+            wait_vmcnt<0>();    // (loads to LDS past the last step)
+            return;
+        }
+        locate();
+        block_barrier();
+    } else {
+        first_stages();
+    }
+
+    // ---- fragments: row l % 16 of X; for the i-th of W, of the wave's columns that which leaves a lane 4 TN consecutive ones of the output
+    const int wm = wave % C::NWM, wn = wave / C::NWM;
+    const int l16 = lane & 15, xr = wm * TM * 16 + l16, wr = wn * 16 * TN + l16 / 4 * 4 * TN + l16 % 4;
+    const int xf_at = xr * 128 + ((lane >> 4) ^ x_key(xr)) * 16;
+    const int wf_at = C::BM * 128 + wr * 128 + ((lane >> 4) ^ w_key_of<TN>(wr)) * 16;    // (rows 4 i on have the same key)
+    auto read = [&](int at, int more, v4i (&f)[2]) {
+        f[0] = *reinterpret_cast<const v4i*>(smem + at + more);
+        f[1] = *reinterpret_cast<const v4i*>(smem + (at ^ 64) + more);
+    };
+    constexpr int RING = TM < 4 ? TM : 4, NEAR = RING / 2;                               // X fragments are read so many of them ahead
+    v4i xf[C::AHEAD ? 2 * TM : RING][2], wf[C::AHEAD ? 2 * TN : TN][2];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) read(xf_at, j * 16 * BK, xf[j]);
+    for (int i = 0; i < TN; ++i) read(wf_at, i * 512, wf[i]);
+#pragma unroll
+    for (int j = 0; j < (C::AHEAD ? TM : NEAR); ++j) read(xf_at, j * 2048, xf[j]);
 
     for (;;) {
         const Rows here = r;       // (the loads move on to the next tile before this one is done)
@@ -363,49 +407,79 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
 #pragma unroll
             for (int i = 0; i < TN; ++i) acc[j][i] = v4i{0, 0, 0, 0};
         auto step = [&]() {
-            const int next = after(stage), fill = stage == 0 ? (S - 1) * C::STAGE : stage - C::STAGE;
-            auto meet = [&]() {
-                wait_vmcnt<(EARLY ? S - 3 : S - 2) * LPS>();
-                if constexpr (!EARLY) wait_lgkmcnt0();    // (early: what was read of the stage before has been multiplied)
-                block_barrier();
-            };
-            if constexpr (EARLY) meet();
-            auto fetch = [&](int q) { read(xf_at + (q < TM ? stage : next), q % TM * 16 * BK, xf[q % RING]); };     // X fragment q from the front of this stage
+            // (two stages) a step's loads go out among the products of the first three X fragments
+            constexpr int SPOTS = 2 * TN * 3, EVERY = SPOTS / LPS;
+            static_assert(FED || (TM > 3 && EVERY > 0), "");
+            const int next = after(stage), fill = fill_of(stage);
+            if constexpr (FED) block_barrier();
+            auto fetch = [&](int q) { read(xf_at + (q < TM ? stage : next), q % TM * 2048, xf[q % RING]); };     // X fragment q from the front of this stage
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
-                if (EARLY || j + AHEAD < TM) fetch(j + AHEAD);
-                if (j == TM - 1 && !EARLY) {
+                if (FED || j + NEAR < TM) fetch(j + NEAR);
+                if (j == TM - 1 && !FED) {
                     ++t;
-                    meet();
+                    wait_vmcnt<0>();
+                    wait_lgkmcnt0();
+                    block_barrier();
 #pragma unroll
-                    for (int q = 0; q < AHEAD; ++q) fetch(TM + q);
+                    for (int q = 0; q < NEAR; ++q) fetch(TM + q);
                 }
 #pragma unroll
-                for (int h = 0; h < H; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < TN; ++i) {
                         acc[j][i] = mfma(wf[i][h], xf[j % RING][h], acc[j][i]);
-                        if (j == TM - 1 && h == H - 1) read(wf_at + next, i * 4 * BK, wf[i]);
-                        const int spot = (j * H + h) * TN + i;
-#pragma unroll
-                        for (int l = 0; l < AT_ONCE; ++l)
-                            if (spot < SPOTS && spot % EVERY == 0 && spot / EVERY * AT_ONCE + l < LPS) issue(fill, spot / EVERY * AT_ONCE + l);
+                        if (j == TM - 1 && h == 1) read(wf_at + next, i * 512, wf[i]);
+                        const int spot = (j * 2 + h) * TN + i;
+                        if (!FED && spot < SPOTS && spot % (EVERY ? EVERY : 1) == 0 && spot / (EVERY ? EVERY : 1) < LPS) issue(fill, spot / (EVERY ? EVERY : 1));
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
-            if constexpr (EARLY) ++t;
             stage = next;
         };
-        int kt = 0;
+        // from the copy c of the fragments' registers, with the next step's read to the other
+        auto step_ahead = [&](auto c) {
+            constexpr int SPOTS = TM * 2 * TN, EVERY = SPOTS / (TM + TN);
+            static_assert(!C::AHEAD || EVERY > 0, "");
+            const int next = after(stage);
+            block_barrier();
+#pragma unroll
+            for (int spot = 0; spot < SPOTS; ++spot) {
+                const int q = spot / (EVERY ? EVERY : 1);
+                if (spot % (EVERY ? EVERY : 1) == 0 && q < TN) read(wf_at + next, q * 512, wf[C::AHEAD ? (1 - c) * TN + q % TN : 0]);
+                else if (spot % (EVERY ? EVERY : 1) == 0 && q < TM + TN) read(xf_at + next, (q - TN) * 2048, xf[C::AHEAD ? (1 - c) * TM + (q - TN) % TM : 0]);
+                const int j = spot / (2 * TN), h = spot / TN % 2, i = spot % TN;
+                acc[j][i] = mfma(wf[C::AHEAD ? c * TN + i : 0][h], xf[C::AHEAD ? c * TM + j : 0][h], acc[j][i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            stage = next;
+        };
+        if constexpr (C::AHEAD) {
 #pragma clang loop unroll(disable)
-        for (int half = 0; half < 2; ++half) {
-            int to = half ? here_steps : here_steps - S + 1;
-            asm volatile("" : "+s"(to));
+            for (int kt = 0; kt + 2 <= here_steps; kt += 2) {
+                step_ahead(std::integral_constant<int, 0>{});
+                step_ahead(std::integral_constant<int, 1>{});
+            }
+            if (here_steps & 1) {
+                step_ahead(std::integral_constant<int, 0>{});
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) xf[j][h] = xf[TM + j][h];
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) wf[i][h] = wf[TN + i][h];
+            }
+        } else {
+            int kt = 0;
 #pragma clang loop unroll(disable)
-            for (; kt < to; ++kt) step();
-            if (half == 0 && tile + (int)gridDim.x < ntiles) {     // the loads of this tile have gone out
-                tile += gridDim.x;
-                begin_tile();
+            for (int half = 0; half < 2; ++half) {
+                int to = FED || half ? here_steps : here_steps - S + 1;
+                asm volatile("" : "+s"(to));
+#pragma clang loop unroll(disable)
+                for (; kt < to; ++kt) step();
+                if (!FED && half == 0) move_on();
             }
         }
         // ---- output: some rows of sixteen at a time through LDS of the wave's own, so that a row leaves as whole lines
@@ -415,7 +489,7 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
         static_assert(ROWS > 0 && 16 / HALVES % ROWS == 0, "");
         const int lane = kept_here((int)threadIdx.x & 63), l16 = lane & 15;
         const float* const scales = reinterpret_cast<const float*>(smem + C::kScales + here_side * C::SCALES);
-        auto key = [](int row) { return PIECES == 8 ? row >> 1 & 7 : row & 15; };      // of a row's pieces
+        auto key = [](int row) { return PIECES == 4 ? row >> 2 & 3 : PIECES == 8 ? row >> 1 & 7 : row & 15; };      // of a row's pieces
         char* const room = smem + C::kRoom + wave * C::ROOM;
         const int row0 = here.begin + wm * TM * 16 + lane / PIECES, col = here_n0 + wn * 16 * TN + lane % PIECES * EACH, have = (int)g.N - col;
         const bool inside = here.begin + (wm + 1) * TM * 16 <= here.end && here_n0 + (wn + 1) * 16 * TN <= (int)g.N;
@@ -470,9 +544,15 @@ __global__ __launch_bounds__(C::NW * 64) void int8_tile_kernel(Int8Args g, int t
                 __builtin_amdgcn_wave_barrier();
             }
         }
-        if (tile == here_tile) break;
+        if constexpr (FED) {
+            tile += gridDim.x;
+            if (tile >= ntiles) break;
+            locate();
+        } else if (tile == here_tile) {
+            break;
+        }
     }
-    wait_vmcnt<0>();    // (loads to LDS past the last step)
+    if constexpr (!FED) wait_vmcnt<0>();    // (loads to LDS past the last step)
 }
 
 template <bool GROUPED, int OUT, typename C>
@@ -483,7 +563,7 @@ hipError_t launch_tile(const Int8Args& g, int parts, int part_blocks, hipStream_
     if (e != hipSuccess) return e;
     const int64_t tiles_m = GROUPED ? g.rows / C::BM + std::min<int64_t>(g.experts, g.rows) : (g.rows + C::BM - 1) / C::BM, tiles_n = (g.N + C::BN - 1) / C::BN;
     const int64_t grid = std::min<int64_t>(tiles_m * tiles_n * parts, (int64_t)compute_units() * (163840 / C::lds()));
-    hipLaunchKernelGGL((int8_tile_kernel<GROUPED, OUT, C>), dim3((unsigned)grid), dim3(C::NW * 64), C::lds(), st, g, (int)tiles_m, (int)tiles_n, parts, part_blocks);
+    hipLaunchKernelGGL((int8_tile_kernel<GROUPED, OUT, C>), dim3((unsigned)grid), dim3((C::NW + C::FEED) * 64), C::lds(), st, g, (int)tiles_m, (int)tiles_n, parts, part_blocks);
     return hipGetLastError();
 }
 
@@ -542,61 +622,57 @@ hipError_t launch_stream(const Int8Args& g, hipStream_t st)
     return hipGetLastError();
 }
 
+typedef Tile<2, 2, 2, 2, 6, 4, true> Tile64;      // 64 x 64
+typedef Tile<4, 2, 2, 2, 6, 4> Tile128n;          // 128 x 64
+typedef Tile<4, 4, 2, 2, 4, 4> Tile128;           // 128 x 128
+typedef Tile<8, 4, 1, 4, 3, 4> Tile128w;          // 128 x 256
+typedef Tile<8, 4, 2, 4, 2, 0> Tile256;           // 256 x 256
+
 // How a product runs.
 struct Plan {
-    int kind = 0;              // 0 .. 4: few rows (rows and columns of a tile below), 5 ..: tiles
+    int kind = 0;              // 0 .. 3: few rows; 4 .. 8: tiles
     int parts = 1, part_blocks = 0;
 };
 
-constexpr int kKinds = 9, kFew = 5;
-constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 64, 128, 256, 256}, kCols[kKinds] = {16, 32, 16, 32, 16, 128, 128, 256, 256};
+constexpr int kKinds = 9, kFew = 4, kMostParts = 8;
+constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 128, 128, 256}, kCols[kKinds] = {16, 32, 16, 32, 64, 64, 128, 256, 256};
 
 Plan plan_int8(const Int8Args& g, bool grouped, size_t room)
 {
     const int forced = options().int8_variant;
+    const int64_t blocks = (g.K + 127) / 128;
     Plan p;
     if (forced) {
         p.kind = (forced - 1) % kKinds;
-        p.parts = grouped || p.kind < kFew ? 1 : 1 << (forced - 1) / kKinds;
-        const int64_t KB = (g.K + 127) / 128;
-        auto each = [&]() { return std::max<int64_t>((KB + p.parts - 1) / p.parts, 4); };
-        while (p.parts > 1 && ((size_t)p.parts * g.rows * g.N * 4 > room || (p.parts - 1) * each() >= KB)) p.parts >>= 1;
+        p.parts = grouped || p.kind < kFew || p.kind > 6 ? 1 : 1 << (forced - 1) / kKinds;
+        auto each = [&]() { return std::max<int64_t>((blocks + p.parts - 1) / p.parts, 6); };
+        while (p.parts > 1 && ((size_t)p.parts * g.rows * g.N * 4 > room || (p.parts - 1) * each() >= blocks)) p.parts >>= 1;
         p.part_blocks = (int)each();
         return p;
     }
-    p.kind = g.rows <= 16 ? 0 : g.rows <= 32 ? 2 : g.rows <= 128 ? 5 : g.rows <= 1024 ? 6 : 7;
+    p.kind = g.rows <= 16 ? 0 : g.rows <= 32 ? 2 : g.rows <= 128 ? 4 : g.rows <= 1024 ? 6 : 8;
     return p;
 }
 
 template <bool GROUPED, int OUT>
 hipError_t launch(const Int8Args& g, const Plan& p, void* partial, hipStream_t st)
 {
-#ifndef T64
-#define T64 2, 4, 2, 2, 128, 4, true
-#define T128 4, 4, 2, 2, 128, 4, true
-#define T256 8, 4, 2, 4, 128, 2
-#define T256B 8, 8, 2, 2, 128, 2
-#endif
-    typedef Tile<T64> Tile64;            // 64 x 128
-    typedef Tile<T128> Tile128;           // 128 x 128
-    typedef Tile<T256> Tile256;           // 256 x 256
-    typedef Tile<T256B> Tile256b;
     if constexpr (!GROUPED) {
         if (p.parts > 1) {
-            if (p.kind == 5) return launch_parts<OUT, Tile64>(g, p.parts, p.part_blocks, partial, st);
-            if (p.kind == 6) return launch_parts<OUT, Tile128>(g, p.parts, p.part_blocks, partial, st);
-            return launch_parts<OUT, Tile256>(g, p.parts, p.part_blocks, partial, st);
+            if (p.kind == 4) return launch_parts<OUT, Tile64>(g, p.parts, p.part_blocks, partial, st);
+            if (p.kind == 5) return launch_parts<OUT, Tile128n>(g, p.parts, p.part_blocks, partial, st);
+            return launch_parts<OUT, Tile128>(g, p.parts, p.part_blocks, partial, st);
         }
     }
     switch (p.kind) {
         case 1: return launch_stream<GROUPED, OUT, Stream<1, 2, 4, 5>>(g, st);
         case 2: return launch_stream<GROUPED, OUT, Stream<2, 1, 4, 5>>(g, st);
         case 3: return launch_stream<GROUPED, OUT, Stream<2, 2, 4, 3>>(g, st);
-        case 4: return launch_stream<GROUPED, OUT, Stream<4, 1, 4, 3>>(g, st);
-        case 5: return launch_tile<GROUPED, OUT, Tile64>(g, 1, 0, st);
+        case 4: return launch_tile<GROUPED, OUT, Tile64>(g, 1, 0, st);
+        case 5: return launch_tile<GROUPED, OUT, Tile128n>(g, 1, 0, st);
         case 6: return launch_tile<GROUPED, OUT, Tile128>(g, 1, 0, st);
-        case 7: return launch_tile<GROUPED, OUT, Tile256>(g, 1, 0, st);
-        case 8: return launch_tile<GROUPED, OUT, Tile256b>(g, 1, 0, st);
+        case 7: return launch_tile<GROUPED, OUT, Tile128w>(g, 1, 0, st);
+        case 8: return launch_tile<GROUPED, OUT, Tile256>(g, 1, 0, st);
         default: break;
     }
     return launch_stream<GROUPED, OUT, Stream<1, 1, 4, 4>>(g, st);
