@@ -635,23 +635,55 @@ struct Plan {
 };
 
 constexpr int kKinds = 9, kFew = 4, kMostParts = 8;
+// a part of K has as many blocks as any of those kinds has stages
+constexpr int kStages[kKinds] = {0, 0, 0, 0, Tile64::S, Tile128n::S, Tile128::S, Tile128w::S, Tile256::S}, kMostStages = 6;
+static_assert(Tile64::S <= kMostStages && Tile128n::S <= kMostStages && Tile128::S <= kMostStages, "");
 constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 128, 128, 256}, kCols[kKinds] = {16, 32, 16, 32, 64, 64, 128, 256, 256};
 
+// What a kind takes, microseconds on a device of `cus` compute units, as fitted to measurements on 256: a start, rounds of tiles, each a fixed part and the steps of K (a quarter of its blocks where four waves share
+// them), but no less than what it reads takes from memory at `rate` TB/s: the weights, once for every row of tiles where rows are few, else both operands once, of the `sets` of weights that have rows.  Parts add the writing,
+// reading and launch of their sum.
+// Measured, each kind and number of parts forced in turn, on 336 products of 1 to 4096 rows with layers from 300 x 9600 to 28672 x 4096 and on 150 drawn ones: the kind that is chosen takes 1.015 of the best one's time in
+// the mean, at worst 1.34 (10 x 9714 x 8400: 21.6 us with tiles of 16 x 32, 16.1 on tiles of 64 x 64); the others up to ten times it (1 x 4096 x 4096: 16 x 16 5.6 us, 64 x 64 9.0, 128 x 128 15; 201 x 10240 x 8192: 128 x 128 27 us,
+// 128 x 64 37, 64 x 64 41, 128 x 256 50; 4096 x 4096 x 4096: 256 x 256 53 us, 128 x 256 63, 128 x 128 65, 64 x 64 100).
+double kind_us(int kind, double rows, double tiles_m, double sets, double N, double K, int64_t blocks, int parts, int cus)
+{
+    static const double start[] = {3.00, 3.16, 2.85, 3.03, 2.71, 2.56, 2.56, 2.54, 1.50}, fixed[] = {0.65, 0.42, 0.56, 0.78, 1.18, 1.74, 2.23, 3.00, 5.90},
+                        step[] = {0.129, 0.350, 0.284, 0.328, 0.183, 0.263, 0.406, 0.854, 1.254}, rate[] = {5.9, 7.35, 6.6, 5.8, 5.9, 6.1, 5.8, 4.1, 3.9};
+    static const int per_cu[] = {2, 3, 1, 1, 1, 1, 1, 1, 1};
+    const bool few = kind < kFew;
+    const double steps = (double)(few ? (blocks + 3) / 4 : std::max<int64_t>((blocks + parts - 1) / parts, kStages[kind]));
+    const double rounds = std::ceil(tiles_m * std::ceil(N / kCols[kind]) * parts / (per_cu[kind] * cus)), bytes = few ? tiles_m * N * K : sets * N * K + rows * K;
+    const double us = start[kind] + std::max(rounds * (fixed[kind] + steps * step[kind]), bytes / (rate[kind] * 1e6 * cus / 256));
+    return parts > 1 ? us + 4.2 + parts * rows * N * 8 / 6.4e6 : us;
+}
+
+// The kind that takes least; in parts only where `room` bytes hold their sums and fewer would leave compute units idle.
 Plan plan_int8(const Int8Args& g, bool grouped, size_t room)
 {
-    const int forced = options().int8_variant;
+    const int forced = options().int8_variant, cus = compute_units();
     const int64_t blocks = (g.K + 127) / 128;
-    Plan p;
-    if (forced) {
-        p.kind = (forced - 1) % kKinds;
-        p.parts = grouped || p.kind < kFew || p.kind > 6 ? 1 : 1 << (forced - 1) / kKinds;
-        auto each = [&]() { return std::max<int64_t>((blocks + p.parts - 1) / p.parts, 6); };
-        while (p.parts > 1 && ((size_t)p.parts * g.rows * g.N * 4 > room || (p.parts - 1) * each() >= blocks)) p.parts >>= 1;
-        p.part_blocks = (int)each();
-        return p;
+    Plan best;
+    double best_us = 1e30;
+    for (int kind = 0; kind < kKinds; ++kind) {
+        if (forced && kind != (forced - 1) % kKinds) continue;
+        // rows of tiles; by expert: as if the rows were spread evenly over the experts, half a tile more to each than they fill
+        const double active = (double)std::min<int64_t>(g.experts, g.rows);
+        const double tiles_m = grouped ? active * std::max(1.0, (double)g.rows / active / kRows[kind] + 0.4) : (double)((g.rows + kRows[kind] - 1) / kRows[kind]);
+        const double tiles = tiles_m * std::ceil((double)g.N / kCols[kind]);
+        for (int parts = 1; parts <= kMostParts; ++parts) {
+            const int64_t each = std::max<int64_t>((blocks + parts - 1) / parts, kMostStages);
+            if (parts > 1 && (grouped || kind < kFew || kind > kFew + 2 || (size_t)parts * g.rows * g.N * 4 > room || (parts - 1) * each >= blocks)) break;
+            if (parts > 1 && !forced && (parts - 1) * tiles >= cus) break;
+            if (forced && parts > 1 << (forced - 1) / kKinds) break;
+            const double us = forced ? (double)-parts : kind_us(kind, (double)g.rows, tiles_m, grouped ? active : 1.0, (double)g.N, (double)g.K, blocks, parts, cus);
+            if (us < best_us) {
+                best = Plan{kind, parts, (int)each};
+                best_us = us;
+            }
+        }
     }
-    p.kind = g.rows <= 16 ? 0 : g.rows <= 32 ? 2 : g.rows <= 128 ? 4 : g.rows <= 1024 ? 6 : 8;
-    return p;
+    return best;
 }
 
 template <bool GROUPED, int OUT>
@@ -665,8 +697,8 @@ hipError_t launch(const Int8Args& g, const Plan& p, void* partial, hipStream_t s
         }
     }
     switch (p.kind) {
-        case 1: return launch_stream<GROUPED, OUT, Stream<1, 2, 4, 5>>(g, st);
-        case 2: return launch_stream<GROUPED, OUT, Stream<2, 1, 4, 5>>(g, st);
+        case 1: return launch_stream<GROUPED, OUT, Stream<1, 2, 2, 3>>(g, st);
+        case 2: return launch_stream<GROUPED, OUT, Stream<2, 1, 4, 3>>(g, st);
         case 3: return launch_stream<GROUPED, OUT, Stream<2, 2, 4, 3>>(g, st);
         case 4: return launch_tile<GROUPED, OUT, Tile64>(g, 1, 0, st);
         case 5: return launch_tile<GROUPED, OUT, Tile128n>(g, 1, 0, st);
@@ -675,7 +707,7 @@ hipError_t launch(const Int8Args& g, const Plan& p, void* partial, hipStream_t s
         case 8: return launch_tile<GROUPED, OUT, Tile256>(g, 1, 0, st);
         default: break;
     }
-    return launch_stream<GROUPED, OUT, Stream<1, 1, 4, 4>>(g, st);
+    return launch_stream<GROUPED, OUT, Stream<1, 1, 4, 3>>(g, st);
 }
 
 }  // namespace
