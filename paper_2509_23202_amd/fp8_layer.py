@@ -1,7 +1,7 @@
-"""A feed-forward layer kept at 8 bits, as a decoder runs it: the residual's addition and the norm leave quantized activations, which one
+"""A feed-forward layer kept at 8 bits (E4M3 codes with a scale per block of 128, or integers with a scale per token and channel), as a decoder runs it: the residual's addition and the norm leave quantized activations, which one
 shared expert and a router's choice of experts multiply; the gated activations are quantized in front of the down projections.
 
-    python -m paper_2509_23202_amd.fp8_layer [--hidden 4096] [--inter 2048] [--experts 32] [--top 4] [--tokens 1 64 2048]
+    python -m paper_2509_23202_amd.fp8_layer [--hidden 4096] [--inter 2048] [--experts 32] [--top 4] [--tokens 1 64 2048] [--format e4m3 | int8] [--routing torch | kernels]
 
 prints for each number of tokens how long the layer takes and how far it is from the same layer in fp32 without quantization.
 """
@@ -13,12 +13,20 @@ from . import binding as fp4
 
 
 class Fp8Layer:
-    """weights: norm [H]; router [E,H]; gate_up [E + 1, 2 I, H] and down [E + 1, H, I], the shared expert's last (all bf16)."""
+    """weights: norm [H]; router [E,H]; gate_up [E + 1, 2 I, H] and down [E + 1, H, I], the shared expert's last (all bf16).
+    routing: None, for a softmax over the chosen experts in torch's operators, or a dict of moe_route's arguments (bias, groups, top_groups, scale, flags), for the choice and the sum of the experts' outputs
+    in the library's kernels."""
 
-    def __init__(self, norm, router, gate_up, down, top: int, eps: float = 1e-6):
-        self.norm, self.router, self.top, self.eps = norm, router, top, eps
+    quantize_weights = staticmethod(fp4.fp8_quantize_weights)
+    norm_quantize = staticmethod(fp4.fp8_rmsnorm_quantize)
+    quantize = staticmethod(fp4.fp8_quantize)
+    gemm = staticmethod(fp4.fp8_gemm)
+    grouped_gemm = staticmethod(fp4.fp8_grouped_gemm)
+
+    def __init__(self, norm, router, gate_up, down, top: int, eps: float = 1e-6, routing=None):
+        self.norm, self.router, self.top, self.eps, self.routing = norm, router, top, eps, routing
         self.experts = router.shape[0]
-        self.gate_up, self.down = fp4.fp8_quantize_weights(gate_up), fp4.fp8_quantize_weights(down)
+        self.gate_up, self.down = self.quantize_weights(gate_up), self.quantize_weights(down)
 
     def _routed(self, operand):
         return tuple(t[: self.experts] for t in operand)
@@ -28,6 +36,9 @@ class Fp8Layer:
 
     def route(self, x):
         """Rows in the experts' order: the token of each, where each expert's begin, each token's rows and weights."""
+        if self.routing is not None:
+            weights, _, tokens, offsets, place = fp4.moe_route(x @ self.router.t(), self.top, **self.routing)
+            return tokens, offsets, place, weights
         weights, chosen = (x @ self.router.t()).float().softmax(1).topk(self.top, dim=1)
         order = torch.argsort(chosen.reshape(-1), stable=True)
         offsets = torch.zeros(self.experts + 1, dtype=torch.int32, device=x.device)
@@ -39,14 +50,29 @@ class Fp8Layer:
     def __call__(self, x, residual):
         """x, residual: bf16 [T,H].  Returns the layer's output and the new residual."""
         normed = torch.empty_like(x)
-        codes, scales, residual = fp4.fp8_rmsnorm_quantize(x, self.norm, self.eps, residual=residual, norm_out=normed)
+        codes, scales, residual = self.norm_quantize(x, self.norm, self.eps, residual=residual, norm_out=normed)
         tokens, offsets, place, weights = self.route(normed)
-        y = fp4.fp8_grouped_gemm(codes, scales, *self._routed(self.gate_up), offsets, rows=tokens)
-        y = fp4.fp8_grouped_gemm(*fp4.fp8_quantize(y, flags=fp4.SILU_MUL), *self._routed(self.down), offsets)
-        shared = fp4.fp8_gemm(codes, scales, *self._shared(self.gate_up))
-        shared = fp4.fp8_gemm(*fp4.fp8_quantize(shared, flags=fp4.SILU_MUL), *self._shared(self.down), flags=fp4.OUT_F32)
+        y = self.grouped_gemm(codes, scales, *self._routed(self.gate_up), offsets, rows=tokens)
+        y = self.grouped_gemm(*self.quantize(y, flags=fp4.SILU_MUL), *self._routed(self.down), offsets)
+        shared = self.gemm(codes, scales, *self._shared(self.gate_up))
+        shared = self.gemm(*self.quantize(shared, flags=fp4.SILU_MUL), *self._shared(self.down), flags=fp4.OUT_F32)
+        if self.routing is not None:
+            return fp4.moe_combine(y, place, weights, shared=shared), residual
         # (every token's rows in the order of its choices: the same sum every time)
         return (shared + (y[place].float() * weights[..., None]).sum(1)).to(torch.bfloat16), residual
+
+
+class Int8Layer(Fp8Layer):
+    """The same layer in 8-bit integers, a scale to each token and each channel."""
+
+    quantize_weights = staticmethod(fp4.int8_quantize)
+    norm_quantize = staticmethod(fp4.int8_rmsnorm_quantize)
+    quantize = staticmethod(fp4.int8_quantize)
+    gemm = staticmethod(fp4.int8_gemm)
+    grouped_gemm = staticmethod(fp4.int8_grouped_gemm)
+
+    def __init__(self, norm, router, gate_up, down, top: int, eps: float = 1e-6, routing=None):
+        super().__init__(norm, router, gate_up, down, top, eps, {"flags": fp4.ROUTE_RENORM} if routing is None else routing)
 
 
 def make_weights(hidden: int, inter: int, experts: int, seed: int, device="cuda"):
@@ -83,9 +109,12 @@ def main():
     for name, value in (("hidden", 4096), ("inter", 2048), ("experts", 32), ("top", 4)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--tokens", type=int, nargs="*", default=[1, 64, 2048])
+    ap.add_argument("--format", choices=["e4m3", "int8"], default="e4m3", help="what operands are quantized to")
+    ap.add_argument("--routing", choices=["torch", "kernels"], default="torch", help="where experts are chosen and their outputs added up (int8: always in the library's kernels)")
     args = ap.parse_args()
     w = make_weights(args.hidden, args.inter, args.experts, 1)
-    layer = Fp8Layer(w["norm"], w["router"], w["gate_up"], w["down"], args.top)
+    layer = (Int8Layer if args.format == "int8" else Fp8Layer)(w["norm"], w["router"], w["gate_up"], w["down"], args.top,
+                                                              routing={"flags": fp4.ROUTE_RENORM} if args.routing == "kernels" else None)
     for T in args.tokens:
         g = torch.Generator(device="cuda")
         g.manual_seed(T)
