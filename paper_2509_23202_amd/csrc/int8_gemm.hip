@@ -228,6 +228,9 @@ __global__ __launch_bounds__(C::WAVES * 64) void int8_stream_kernel(Int8Args g, 
 // free.  AHEAD: all fragments of the next step are read while this one's are multiplied, into a second copy of their registers; else the W fragments stay, and the X fragments pass through a few buffers.
 //   Without them (256 x 256, which has no registers for more than eight waves) the waves that multiply load, and there are two stages: before its last X fragment a wave has read all it needs of the stage.  There it
 // waits for its loads of the next one, the workgroup meets, and the last fragment's products cover the reads of the next step's first fragments.
+// The two waves of a SIMD have different rows: one that has none in this tile leaves the other the SIMD (16384 rows dealt by a router to 64 experts 4096 x 4096, 97 tiles of which 35 are at most half full: 415 -> 399 us).
+// What is left there is the weights: experts with 256 rows each take 290 us, of which reading 64 of them at 6.3 TB/s would be 170 and multiplying, as one expert's rows, 204; asking for each line a step earlier made
+// it 302, rows of another pitch (K 3968 to 4352) changed nothing.
 //   A tile takes S steps at least: the meeting in a step that is not one of its last S - 1 stands between a tile's output, which reads its scales, and the loads of the scales two tiles on.
 template <int TM_, int TN_, int NWM_, int NWN_, int STAGES_, int FEED_, bool AHEAD_ = false>
 struct Tile {
@@ -383,7 +386,7 @@ __global__ __launch_bounds__((C::NW + C::FEED) * 64) void int8_tile_kernel(Int8A
     }
 
     // ---- fragments: row l % 16 of X; for the i-th of W, of the wave's columns that which leaves a lane 4 TN consecutive ones of the output
-    const int wm = wave % C::NWM, wn = wave / C::NWM;
+    const int wm = wave / C::NWN, wn = wave % C::NWN;
     const int l16 = lane & 15, xr = wm * TM * 16 + l16, wr = wn * 16 * TN + l16 / 4 * 4 * TN + l16 % 4;
     const int xf_at = xr * 128 + ((lane >> 4) ^ x_key(xr)) * 16;
     const int wf_at = C::BM * 128 + wr * 128 + ((lane >> 4) ^ w_key_of<TN>(wr)) * 16;    // (rows 4 i on have the same key)
@@ -401,6 +404,7 @@ __global__ __launch_bounds__((C::NW + C::FEED) * 64) void int8_tile_kernel(Int8A
     for (;;) {
         const Rows here = r;       // (the loads move on to the next tile before this one is done)
         const int here_n0 = n0, here_tile = tile, here_part = part, here_side = side, here_steps = steps;
+        const bool without = !FED && here.begin + wm * TM * 16 >= here.end;
         v4i acc[TM][TN];
 #pragma unroll
         for (int j = 0; j < TM; ++j)
@@ -435,6 +439,16 @@ __global__ __launch_bounds__((C::NW + C::FEED) * 64) void int8_tile_kernel(Int8A
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
+            stage = next;
+        };
+        // (two stages) of a wave that has no rows in this tile
+        auto step_without = [&]() {
+            const int next = after(stage), fill = fill_of(stage);
+#pragma unroll
+            for (int i = 0; i < LPS; ++i) issue(fill, i);
+            ++t;
+            wait_vmcnt<0>();
+            block_barrier();
             stage = next;
         };
         // from the copy c of the fragments' registers, with the next step's read to the other
@@ -477,9 +491,22 @@ __global__ __launch_bounds__((C::NW + C::FEED) * 64) void int8_tile_kernel(Int8A
             for (int half = 0; half < 2; ++half) {
                 int to = FED || half ? here_steps : here_steps - S + 1;
                 asm volatile("" : "+s"(to));
+                if (without) {
 #pragma clang loop unroll(disable)
-                for (; kt < to; ++kt) step();
+                    for (; kt < to; ++kt) step_without();
+                } else {
+#pragma clang loop unroll(disable)
+                    for (; kt < to; ++kt) step();
+                }
                 if (!FED && half == 0) move_on();
+            }
+            if (without) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) read(wf_at + stage, i * 512, wf[i]);
+#pragma unroll
+                for (int q = 0; q < NEAR; ++q) read(xf_at + stage, q * 2048, xf[q]);
+                if (tile == here_tile) break;
+                continue;
             }
         }
         // ---- output: some rows of sixteen at a time through LDS of the wave's own, so that a row leaves as whole lines
