@@ -269,14 +269,21 @@ __device__ __forceinline__ bool any_lane(bool v)
     return lanes_max<LANES>((uint32_t)v) != 0;
 }
 
-// The choice by exact scores, with the keys in LDS: for tokens whose scores fp32 cannot tell apart.  Lane j is left the j-th expert, or -1.
-template <int LANES, bool F32>
-__device__ __forceinline__ int choose_exactly(const RouteArgs& a, int lane, int64_t at, float most, double sum, bool bad, u64* keys)
+// The choice by exact scores, by a whole wave with the keys in LDS: for tokens whose scores fp32 cannot tell apart.  Lane j is left the j-th expert, or -1.
+template <bool F32>
+__device__ __forceinline__ int choose_exactly(const RouteArgs& a, int64_t at, float most, u64* keys)
 {
-    const Token<LANES, F32> k{a, lane, at, most, sum};
+    constexpr int LANES = 64;
+    const int lane = threadIdx.x & 63;
+    Token<LANES, F32> k{a, lane, at, most, 1.0};
+    if (!a.sigmoid) {
+        double sum = 0.0;
+        for (int e = lane; e < a.experts; e += LANES) sum += k.exact_power(k.logit(e));
+        k.sum = lanes_sum<LANES>(sum);
+    }
     for (int e = lane; e < a.experts; e += LANES) {
         const float z = k.logit(e), b = a.bias ? a.bias[e] : 0.0f;
-        keys[e] = z == -__builtin_inff() || b == -__builtin_inff() || bad ? 0 : order_of(k.exact_score(z) + (double)b);
+        keys[e] = z == -__builtin_inff() || b == -__builtin_inff() ? 0 : order_of(k.exact_score(z) + (double)b);
     }
     __builtin_amdgcn_wave_barrier();
     u64 kept = ~0ull;
@@ -411,13 +418,13 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool 
         for (int i = 0; i < EACH; ++i) next = max(next, key[i]);
         next = lanes_max<LANES>(next);
         sure &= next == 0 || apart(before, of_order(next), doubt);
-        if (__any(real && !sure)) {
-            if (!a.sigmoid) {
-                double sum = 0.0;
-                for (int e = lane; e < a.experts; e += LANES) sum += k.exact_power(k.logit(e));
-                k.sum = lanes_sum<LANES>(sum);
-            }
-            mine = choose_exactly<LANES, F32>(a, lane, k.at, k.most, k.sum, bad, keys);
+        for (u64 unsure = __ballot(real && !sure && lane == 0); unsure; unsure &= unsure - 1) {      // (a token that is bad has no keys, of which it is sure)
+            const int of = __builtin_ctzll(unsure), wave_lane = (int)threadIdx.x & 63;
+            const int64_t at = (int64_t)((u64)(uint32_t)__builtin_amdgcn_readlane((int)(k.at >> 32), of) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k.at, of));
+            const int exact = choose_exactly<F32>(a, at, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k.most), of)), keys - (wave_lane - lane) * EACH);
+            const int j = __builtin_amdgcn_ds_bpermute(lane * 4, exact);
+            if (wave_lane - lane == of) mine = j;
+            __builtin_amdgcn_wave_barrier();
         }
         of_mine = mine >= 0 ? k.logit(mine) : 0.0f;
     }
