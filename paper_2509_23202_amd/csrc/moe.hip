@@ -166,7 +166,7 @@ struct Token {
     {
         if (a.sigmoid) return sigmoid_of(z);
         const float x = z - most, back = x - z;
-        return power_of_e(fmaxf(x, -200.0f), (z - (x - back)) + (-most - back));      // (what the subtraction has rounded off)
+        return x > -200.0f ? power_of_e(x, (z - (x - back)) + (-most - back)) : 0.0f;      // (with what the subtraction has rounded off)
     }
     __device__ static float sigmoid_of(float z) { return z < -87.3f ? 0.0f : 1.0f / (1.0f + power_of_e(fmaxf(-z, -200.0f))); }
 };

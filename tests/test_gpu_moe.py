@@ -110,6 +110,29 @@ def test_masks_equal_logits_and_numbers_that_are_not_finite(fp4, biased, sigmoid
             assert torch.isnan(w).all() and (e == -1).all() and (offsets == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("E,top,groups", [(8, 8, 1), (70, 16, 7), (256, 20, 8)])
+def test_the_largest_and_lowest_logits_and_biases(fp4, dtype, E, top, groups):
+    """Masks of the type's lowest value beside its largest one, whose difference is beyond the type, and biases beside which a score counts for nothing."""
+    say(f"largest and lowest E={E} {dtype}")
+    z = logits(40, E, E, dtype).clone()
+    end = torch.finfo(dtype)
+    z[0] = end.min
+    z[1] = end.max
+    z[2, ::2] = end.min
+    z[3, 1:] = end.min
+    z[4, 1::2], z[4, ::2] = end.max, end.min
+    z[5, 3] = end.max
+    z[6, 3] = end.min
+    z[7] = -87.0 - torch.arange(E, device="cuda") % 3
+    bias = torch.zeros(E, device="cuda")
+    bias[1], bias[2], bias[4], bias[5] = 3e38, -3e38, 1e30, 3e38
+    rising = torch.linspace(-3e38, 3e38, E, device="cuda")
+    for sigmoid, renorm, b in itertools.product((0, fp4.ROUTE_SIGMOID), (0, fp4.ROUTE_RENORM), (None, bias, rising)):
+        for g in {1, groups}:
+            check(fp4, z, top, bias=b, groups=g, top_groups=(g + 1) // 2 if top <= E // g * ((g + 1) // 2) else g, flags=sigmoid | renorm)
+
+
 @pytest.mark.parametrize("T", [16384, 30011])
 def test_many_tokens(fp4, T):
     """Plain torch in 64 bits on the device: experts in descending order of their choice, a stable sort."""
