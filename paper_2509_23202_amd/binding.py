@@ -645,6 +645,7 @@ def moe_route(logits, top: int, *, bias=None, groups: int = 1, top_groups: int =
     T, E = logits.shape
     assert logits.stride(1) == 1 or E <= 1
     stride = logits.stride(0) if T > 1 else E
+    assert logits.dtype == torch.float32 or not flags & INPUT_F32
     if logits.dtype == torch.float32:
         flags |= INPUT_F32
     if bias is not None:
@@ -675,8 +676,10 @@ def moe_combine(y, places, weights, *, shared=None, flags: int = 0, out=None):
     _is_tensor(y, y.dtype, R, H)
     _is_tensor(places, torch.int32, T, top)
     _is_tensor(weights, torch.float32, T, top)
+    assert y.dtype == torch.float32 or not flags & INPUT_F32
     if y.dtype == torch.float32:
         flags |= INPUT_F32
+    assert not flags & SHARED_F32 or (shared is not None and shared.dtype == torch.float32)
     if shared is not None:
         assert shared.dtype in (torch.bfloat16, torch.float32)
         _is_tensor(shared, shared.dtype, T, H)

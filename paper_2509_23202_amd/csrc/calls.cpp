@@ -440,7 +440,7 @@ PyObject* route(PyObject*, PyObject* const* args, Py_ssize_t n)
         Py_RETURN_NONE;
     const int64_t T = z->size(0), E = z->size(1);
     const bool f32 = z->scalar_type() == at::kFloat;
-    if ((!f32 && z->scalar_type() != at::kBFloat16) || T <= 0 || E <= 0 || z->stride(1) != 1 || top <= 0 || top > E || T > (1ll << 24) ||
+    if ((!f32 && (z->scalar_type() != at::kBFloat16 || (flags & FP4MR_INPUT_F32))) || T <= 0 || E <= 0 || z->stride(1) != 1 || top <= 0 || top > E || T > (1ll << 24) ||
         (bias && (bias->scalar_type() != at::kFloat || bias->dim() != 1 || bias->size(0) != E || !bias->is_contiguous())))
         Py_RETURN_NONE;
     const at::Tensor weights = empty({T, top}, at::kFloat, *z), experts = empty({T, top}, at::kInt, *z), rows = empty({T * top}, at::kInt, *z), offsets = empty({E + 1}, at::kInt, *z),

@@ -279,3 +279,15 @@ def test_refusals_of_the_binding(fp4):
                  lambda: fp4.moe_route(torch.zeros(2, 1025, device="cuda"), 2), lambda: fp4.moe_route(torch.zeros(2, 128, device="cuda"), 65)):
         with pytest.raises(fp4.Fp4mrError):
             call()
+
+
+def test_flags_that_name_a_type_have_to_be_the_tensors(fp4):
+    """Of the compiled calls too, which hand such calls on to the binding."""
+    z = logits(4, 16, 1, torch.bfloat16)
+    w, e, r, o, p = fp4.moe_route(z, 2)
+    y = torch.zeros(8, 32, device="cuda", dtype=torch.bfloat16)
+    for call in (lambda: fp4.moe_route(z, 2, flags=fp4.INPUT_F32), lambda: fp4.moe_combine(y, p, w, flags=fp4.INPUT_F32), lambda: fp4.moe_combine(y, p, w, shared=y[:4], flags=fp4.SHARED_F32)):
+        with pytest.raises(AssertionError):
+            call()
+    assert torch.equal(fp4.moe_route(z.float(), 2, flags=fp4.INPUT_F32)[1], e)
+    assert torch.equal(fp4.moe_combine(y.float(), p, w, flags=fp4.INPUT_F32), fp4.moe_combine(y, p, w))

@@ -122,3 +122,31 @@ def test_workspaces_are_device_memory_of_their_own_size(b, monkeypatch):
         assert not calls
         run(room(1 << 20).as_subclass(OnDevice))
         assert len(calls) == 1 and 1 << 20 in calls.pop()
+
+
+def test_flags_that_name_a_type_have_to_be_the_tensors(b, monkeypatch):
+    """A flag that says that bf16 tensors are fp32 would have the device read twice what they hold: refused in front of the library, also by the compiled calls, which hand such calls on."""
+    import torch
+
+    class OnDevice(torch.Tensor):       # (host memory that says it is the device's: nothing is launched)
+        is_cuda = True
+        device = torch.device("cuda", 0)
+
+    calls = []
+    monkeypatch.setattr(b, "_stream", lambda: 0)
+    monkeypatch.setattr(b, "_current_device", lambda: 0)
+    monkeypatch.setattr(b, "_calls", None)
+    monkeypatch.setattr(b, "_new", lambda like, shape, dtype: torch.empty(shape, dtype=dtype).as_subclass(OnDevice))
+    on = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype).as_subclass(OnDevice)
+    for name in ("moe_route", "moe_combine"):
+        monkeypatch.setattr(b.lib, name, lambda *a: calls.append(a) or 0)
+    half, places = torch.bfloat16, on(4, 2, dtype=torch.int32)
+    for run in (lambda: b.moe_route(on(4, 32, dtype=half), 2, flags=b.INPUT_F32), lambda: b.moe_combine(on(8, 32, dtype=half), places, on(4, 2), flags=b.INPUT_F32),
+                lambda: b.moe_combine(on(8, 32, dtype=half), places, on(4, 2), shared=on(4, 32, dtype=half), flags=b.SHARED_F32),
+                lambda: b.moe_combine(on(8, 32, dtype=half), places, on(4, 2), flags=b.SHARED_F32)):
+        with pytest.raises(AssertionError):
+            run()
+    assert not calls
+    b.moe_route(on(4, 32), 2, flags=b.INPUT_F32)
+    b.moe_combine(on(8, 32), places, on(4, 2), shared=on(4, 32), flags=b.INPUT_F32 | b.SHARED_F32)
+    assert len(calls) == 2
