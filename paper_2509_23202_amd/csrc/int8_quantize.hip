@@ -182,8 +182,9 @@ __global__ __launch_bounds__(T) void int8_rmsnorm_kernel(NormArgs a)
         widen8(w[c], f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * f[i];
-        if (a.norm_out && col < a.K) store8(a.norm_out + row * a.K + col, v[c]);
-        m = max(m, amax8(v[c]));          // (past the row's end its last eight again)
+        if (col >= a.K) continue;          // (past the row's end its last eight were read again, perhaps after another wave has stored their sums there)
+        if (a.norm_out) store8(a.norm_out + row * a.K + col, v[c]);
+        m = max(m, amax8(v[c]));
     }
     const float amax = __uint_as_float(max(block_max<T>(m, part_max), kAmaxLeast)), inv = kTop * (1.0f / amax);
 #pragma unroll

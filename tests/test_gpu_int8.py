@@ -411,3 +411,16 @@ def test_refusals_of_the_binding(fp4):
                  lambda: fp4.int8_rmsnorm_quantize(x, x[0].contiguous(), residual_out=torch.empty_like(x))):
         with pytest.raises(fp4.Fp4mrError):
             call()
+
+
+@pytest.mark.parametrize("K", [80, 528, 4112, 8208, 16400, 40000])
+def test_rmsnorm_into_what_it_adds_with_rows_that_leave_threads_idle(fp4, K):
+    """The sum may take the place of the residual or of x: with rows that are a little longer than a number of threads, idle ones read what others store."""
+    rows = 2048
+    x, r = bf16(rows, K, 1), bf16(rows, K, 2)
+    w = bf16(1, K, 3)[0].contiguous()
+    want = fp4.int8_rmsnorm_quantize(x, w, residual=r)
+    for place in ("residual", "x"):
+        xi, ri = x.clone(), r.clone()
+        got = fp4.int8_rmsnorm_quantize(xi, w, residual=ri, residual_out=ri if place == "residual" else xi)
+        assert all(torch.equal(g, t) for g, t in zip(got, want)), place
