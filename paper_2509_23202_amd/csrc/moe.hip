@@ -138,9 +138,9 @@ __device__ __forceinline__ float power_of_e(float x, float lo = 0.0f)
 // How the experts are compared: a bf16 logit and the index in one word, an fp32 logit, or a score.
 enum { kPacked, kLogit, kScore };
 
-// A score in fp32, from an exponential within two steps, sums in binary64 and a division, is within 2^-20 of the score: of softmax (x = z - max) s (2^-22 + 2^-22 + 2^-23) + s 2^-24 sum e^x |x| / sum e^x + 0.37 2^-24, where s
-// times the quotient of sums is less than 2, of sigmoid less.  With its bias it is within 2^-20 + 2^-24 (1 + |bias|), a sum of two of them within twice 2^-20 + 2^-23 (1 + the largest |bias|), the doubt.  Two that are
-// further apart than twice their doubt are in the order of their exact values.
+// A score in fp32, from an exponential within two steps, sums in binary64 and a reciprocal, is within 2^-20 of the score: of softmax (x = z - max) s (2^-22 + 2^-22 + 2^-23 + 2^-24) + s 2^-24 sum e^x |x| / sum e^x
+// + 0.37 2^-24, where s times the quotient of sums is less than 2 (0.84 2^-20 in all), of sigmoid s (2^-22 + 2^-24 + 2^-23) + 0.28 2^-24.  With its bias it is within 2^-20 + 2^-24 (1 + |bias|), a sum of two of them
+// within twice 2^-20 + 2^-23 (1 + the largest |bias|), the doubt.  Two that are further apart than twice their doubt are in the order of their exact values.
 __device__ __forceinline__ bool apart(float larger, float smaller, float doubt) { return larger - smaller > 2.0f * doubt; }
 
 // A token's LANES lanes' view of what is the same for all of them.
@@ -160,15 +160,14 @@ struct Token {
     __device__ double exact_power(float z) const { return z == -__builtin_inff() ? 0.0 : exp((double)z - (double)most); }
     __device__ double exact_score(float z) const { return !a.sigmoid ? exact_power(z) / sum : z == -__builtin_inff() ? 0.0 : 1.0 / (1.0 + exp(-(double)z)); }
     // in fp32, of softmax before the division by the sum; what is below 2^-126 is 0
-    __device__ float score(float z) const { return a.sigmoid ? sigmoid_of(z) : power_of_e(fmaxf(z - most, -200.0f)); }
+    __device__ float score(float z) const { return a.sigmoid ? z < -87.3f ? 0.0f : __builtin_amdgcn_rcpf(1.0f + power_of_e(fmaxf(-z, -200.0f))) : power_of_e(fmaxf(z - most, -200.0f)); }
     // the same where the last bits of z - most count too
     __device__ float weight(float z) const
     {
-        if (a.sigmoid) return sigmoid_of(z);
+        if (a.sigmoid) return z < -87.3f ? 0.0f : 1.0f / (1.0f + power_of_e(fmaxf(-z, -200.0f)));
         const float x = z - most, back = x - z;
         return x > -200.0f ? power_of_e(x, (z - (x - back)) + (-most - back)) : 0.0f;      // (with what the subtraction has rounded off)
     }
-    __device__ static float sigmoid_of(float z) { return z < -87.3f ? 0.0f : 1.0f / (1.0f + power_of_e(fmaxf(-z, -200.0f))); }
 };
 
 // The best top_groups groups, as bits.  key: a function of the expert.  sure: stays so where keys in fp32, each within `doubt`, leave none.
@@ -345,11 +344,12 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool 
 
     // ---- keys
     uint32_t key[EACH];
+    const float part = 1.0f / (float)k.sum;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const bool out = z[i] == -__builtin_inff() || bad;
         if constexpr (BY == kScore) {
-            const float s = a.sigmoid ? k.score(z[i]) : k.score(z[i]) / (float)k.sum;
+            const float s = a.sigmoid ? k.score(z[i]) : k.score(z[i]) * part;
             key[i] = out || b[i] == -__builtin_inff() ? 0 : order_of(s + b[i]);
         } else if constexpr (BY == kPacked) {     // (of a bf16 the order's low half says nothing; of equal ones the first is the largest)
             key[i] = out ? 0 : (order_of(z[i]) & 0xffff0000u) | (uint32_t)(0xffff - (LANES * i + lane));
@@ -713,10 +713,11 @@ FastDiv fast_div_by(uint32_t d)
     return f;
 }
 
-// Tokens of a run and runs.
+// Tokens of a run and runs.  At least eight, a workgroup of eight waves: runs of four leave twice the counts to add (1024 tokens, 256 experts 12.1 us, with eight 10.9), of sixteen half the compute units
+// idle where tokens are few (256 of 256 experts in groups 12.5, 12.3, 15.3 us).
 void runs_of(int64_t tokens, int& run, int& runs)
 {
-    run = (int)std::max<int64_t>(4, (tokens + kMaxRuns - 1) / kMaxRuns);
+    run = (int)std::max<int64_t>(8, (tokens + kMaxRuns - 1) / kMaxRuns);
     runs = (int)((tokens + run - 1) / run);
 }
 
