@@ -339,6 +339,8 @@ fp4mr_status_t fp4_dequantize(const void* codes, const void* scales, const float
  *                           instructions (same results bit for bit; abs-max and 4/3 policies only)
  *   FP4MR_OPT_FP8_VARIANT   0 (default): fp8_gemm and fp8_grouped_gemm pick their kernel; 1..7: force one of few rows or of tiles, 8..13: fp8_gemm in
  *                           2, 4 or 8 parts of K where the workspace holds their sums (products that a forced kernel does not take run on another)
+ *   FP4MR_OPT_INT8_VARIANT  0 (default): int8_gemm and int8_grouped_gemm pick their kernel; 1..9: force one, 10..18, 19..27, 28..36: the same in 2, 4 and 8 parts
+ *                           of K, or as many as the kernel, the workspace and K have room for (the same results bit for bit)
  */
 enum { FP4MR_OPT_GEMM_VARIANT = 0, FP4MR_OPT_GEMM_GRID = 1, FP4MR_OPT_SW_CODEC = 2, FP4MR_OPT_FP8_VARIANT = 3, FP4MR_OPT_INT8_VARIANT = 4 };
 fp4mr_status_t fp4_set_option(int option, int value);
@@ -456,7 +458,7 @@ fp4mr_status_t int8_quantize(const void* x, int64_t x_stride, int64_t M, int64_t
  * out[m,n] = (float(sum_k a[m,k] w[n,k]) * a_scales[m]) * w_scales[n]: the sum is exact, float() rounds it to the nearest binary32, and both multiplications are binary32's.  out is bf16
  * (one more rounding), or fp32 with FP4MR_OUT_F32.  No plan, workspace or kernel changes a bit of it.
  *   workspace    optional: with int8_workspace_bytes(M, N, K) bytes (0 where that is of no use) a product of few tiles and a long K is split along K over otherwise
- *                idle compute units, and its parts' sums are kept there.  With less, or NULL, it runs in fewer parts, or in one.
+ *                idle compute units, and its parts' sums are kept there.  With less, or NULL, it runs in fewer parts, or in one.  Calls that may run at the same time need one each.
  */
 fp4mr_status_t int8_gemm(const void* a_codes, const float* a_scales, const void* w_codes, const float* w_scales, int64_t M, int64_t N,
                          int64_t K, void* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
@@ -483,7 +485,7 @@ fp4mr_status_t int8_grouped_gemm(const void* a_codes, const float* a_scales, int
  *   rows_out     int32, room for [T * top]: the token of each row, the rows of expert 0 first, an expert's in the order of the tokens.  What lies behind the last row is not written.
  *   offsets_out  int32 [experts + 1]: expert e has rows offsets[e] .. offsets[e+1] - 1
  *   places_out   int32 [T,top]: the row of each choice, -1 where there is none
- *   workspace    moe_workspace_bytes(T, experts, top) bytes, 16-byte aligned
+ *   workspace    moe_workspace_bytes(T, experts, top) bytes (0 for few choices: then it may be NULL), 16-byte aligned; what it holds means nothing between calls, but calls that may run at the same time need one each
  * T <= 2^24, T * top <= 2^30, experts <= 1024, top <= 64 and <= experts / groups * top_groups, groups <= 64 and a divisor of experts.  Tensors need the alignment of their elements only.  T = 0 writes offsets_out.
  * Outputs must not overlap inputs or each other.
  */

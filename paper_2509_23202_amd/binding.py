@@ -693,7 +693,7 @@ def moe_combine(y, places, weights, *, shared=None, flags: int = 0, out=None):
 
 
 def set_option(option: int, value: int) -> None:
-    """Process-wide tuning / cross-check switch (OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC); 0 restores the default."""
+    """Process-wide tuning / cross-check switch (OPT_GEMM_VARIANT, OPT_GEMM_GRID, OPT_SW_CODEC, OPT_FP8_VARIANT, OPT_INT8_VARIANT); 0 restores the default."""
     _check(lib.fp4_set_option(int(option), int(value)))
 
 
