@@ -424,3 +424,37 @@ def test_rmsnorm_into_what_it_adds_with_rows_that_leave_threads_idle(fp4, K):
         xi, ri = x.clone(), r.clone()
         got = fp4.int8_rmsnorm_quantize(xi, w, residual=ri, residual_out=ri if place == "residual" else xi)
         assert all(torch.equal(g, t) for g, t in zip(got, want)), place
+
+
+def test_rows_and_outputs_beyond_32_bits(fp4):
+    """Elements of an output and of a quantizer's input past 2^32 and 2^31."""
+    M, N, K = 70000, 65552, 128
+    say("int8 gemm of 4.6e9 outputs")
+    (a, sa), (w, sw) = R.operand(M, K, 1), R.operand(N, K, 2)
+    out = fp4.int8_gemm(a, sa, w, sw)
+    m, n = torch.tensor([0, 32767, 65535, 65536, M - 1], device="cuda"), torch.tensor([0, 255, 65535, N - 1], device="cuda")
+    assert torch.equal(out[m][:, n].cpu(), R.product(a[m], sa[m], w[n], sw[n], torch.bfloat16))
+    del out
+    say("int8 quantize of 2.5e9 elements")
+    x = torch.zeros(150000, 16400, dtype=torch.bfloat16, device="cuda")
+    x[-2:] = bf16(2, 16400, 3)
+    codes, scales = fp4.int8_quantize(x)
+    c, s = fp4.int8_quantize(x[-2:].clone())
+    assert torch.equal(codes[-2:], c) and torch.equal(scales[-2:], s) and (codes[:-2] == 0).all() and (scales[:-2] == float(np.float32(2.0 ** -100) / np.float32(127))).all()
+
+
+@pytest.mark.parametrize("M,N,parts", [(64, 512, False), (33, 4096, True)])
+def test_two_streams_at_once(fp4, M, N, parts):
+    """Products, also in parts of K, each call with a workspace of its own, and quantizers, on two streams that wait for nothing of each other's."""
+    sets = [(bf16(M, 14336, 40 + i).contiguous(), *R.operand(N, 14336, 50 + i, 0.01)) for i in range(2)]
+    assert (fp4.int8_workspace_bytes(M, N, 14336) > 0) == parts
+    want = [fp4.int8_gemm(*fp4.int8_quantize(x), w, sw) for x, w, sw in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sets], [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                x, w, sw = sets[i]
+                got[i].append(fp4.int8_gemm(*fp4.int8_quantize(x), w, sw))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i]) for i in range(2) for g in got[i])

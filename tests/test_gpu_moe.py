@@ -291,3 +291,54 @@ def test_flags_that_name_a_type_have_to_be_the_tensors(fp4):
             call()
     assert torch.equal(fp4.moe_route(z.float(), 2, flags=fp4.INPUT_F32)[1], e)
     assert torch.equal(fp4.moe_combine(y.float(), p, w, flags=fp4.INPUT_F32), fp4.moe_combine(y, p, w))
+
+
+def test_rows_and_outputs_beyond_32_bits(fp4):
+    say("combine from 4.6e9 elements, and to as many")
+    R_, H = 70000, 65544
+    y = torch.zeros(R_, H, dtype=torch.bfloat16, device="cuda")
+    y[-3:] = torch.randn(3, H, device="cuda").to(torch.bfloat16)
+    places = torch.tensor([[R_ - 1, 0], [R_ - 3, R_ - 2]], dtype=torch.int32, device="cuda")
+    weights = torch.tensor([[0.5, 1.0], [2.0, 0.25]], device="cuda")
+    few = y[-3:].clone()
+    small = torch.tensor([[2, -1], [0, 1]], dtype=torch.int32, device="cuda")
+    assert torch.equal(fp4.moe_combine(y, places, weights), fp4.moe_combine(few, small, weights))
+    del y
+    many = torch.randint(0, 3, (R_, 1), dtype=torch.int32, device="cuda")
+    out = fp4.moe_combine(few, many, torch.ones(R_, 1, device="cuda"))
+    assert all(torch.equal(out[i : i + 5000], few[many[i : i + 5000, 0].long()]) for i in range(0, R_, 5000))
+    del out
+    out = fp4.moe_combine(few[:, 1:8].contiguous(), many, torch.ones(R_, 1, device="cuda"))
+    assert torch.equal(out, few[many[:, 0].long(), 1:8])
+
+
+def test_two_streams_at_once_and_two_graphs(fp4):
+    """Both launches of a route, each call with a workspace of its own, on two streams that wait for nothing of each other's; then both recorded, with a workspace each, and replayed at once."""
+    T, E, top = 700, 96, 6
+    zs = [logits(T, E, 60 + i) for i in range(2)]
+    assert fp4.moe_workspace_bytes(T, E, top) > 0
+    want = [fp4.moe_route(z, top) for z in zs]
+    rows = [int(w[3][-1]) for w in want]
+    same = lambda got, i: all(torch.equal(g[: rows[i]] if g.dim() == 1 and g.numel() == T * top else g, w[: rows[i]] if w.dim() == 1 and w.numel() == T * top else w) for g, w in zip(got, want[i]))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in zs], [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(fp4.moe_route(zs[i], top))
+    torch.cuda.synchronize()
+    assert all(same(g, i) for i in range(2) for g in got[i])
+    graphs, held = [torch.cuda.CUDAGraph() for _ in zs], []
+    rooms = [torch.empty(fp4.moe_workspace_bytes(T, E, top), dtype=torch.uint8, device="cuda") for _ in zs]
+    for i, s in enumerate(streams):
+        with torch.cuda.stream(s), torch.cuda.graph(graphs[i], stream=s):
+            held.append(fp4.moe_route(zs[i], top, workspace=rooms[i]))
+    for _ in range(5):
+        for t in (t for h in held for t in h):
+            t.zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(same(h, i) for i, h in enumerate(held))

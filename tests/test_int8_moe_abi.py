@@ -150,3 +150,33 @@ def test_flags_that_name_a_type_have_to_be_the_tensors(b, monkeypatch):
     b.moe_route(on(4, 32), 2, flags=b.INPUT_F32)
     b.moe_combine(on(8, 32), places, on(4, 2), shared=on(4, 32), flags=b.INPUT_F32 | b.SHARED_F32)
     assert len(calls) == 2
+
+
+def test_tensors_of_another_device_are_refused(b, monkeypatch):
+    """Kernels run on the current device: tensors of another one are refused in front of the library."""
+    import torch
+
+    class OnDevice(torch.Tensor):       # (host memory that says it is a device's: nothing is launched)
+        is_cuda = True
+        device = torch.device("cuda", 1)
+
+    calls = []
+    monkeypatch.setattr(b, "_stream", lambda: 0)
+    monkeypatch.setattr(b, "_current_device", lambda: 0)
+    monkeypatch.setattr(b, "_calls", None)
+    monkeypatch.setattr(b, "_new", lambda like, shape, dtype: torch.empty(shape, dtype=dtype).as_subclass(OnDevice))
+    on = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype).as_subclass(OnDevice)
+    i8, i32, half = torch.int8, torch.int32, torch.bfloat16
+    runs = {"int8_quantize": lambda: b.int8_quantize(on(4, 32, dtype=half)), "int8_rmsnorm_quantize": lambda: b.int8_rmsnorm_quantize(on(4, 32, dtype=half), on(32, dtype=half)),
+            "int8_gemm": lambda: b.int8_gemm(on(4, 32, dtype=i8), on(4), on(8, 32, dtype=i8), on(8)),
+            "int8_grouped_gemm": lambda: b.int8_grouped_gemm(on(4, 32, dtype=i8), on(4), on(2, 8, 32, dtype=i8), on(2, 8), on(3, dtype=i32)),
+            "moe_route": lambda: b.moe_route(on(4, 32), 2), "moe_combine": lambda: b.moe_combine(on(8, 32), on(4, 2, dtype=i32), on(4, 2))}
+    for name, run in runs.items():
+        monkeypatch.setattr(b.lib, name, lambda *a: calls.append(a) or 0)
+        with pytest.raises(AssertionError):
+            run()
+        assert not calls, name
+    OnDevice.device = torch.device("cuda", 0)
+    for run in runs.values():
+        run()
+    assert len(calls) == 6
