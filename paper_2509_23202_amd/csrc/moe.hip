@@ -10,7 +10,7 @@
 // The chosen pairs (token, place among its choices) are then sorted by expert, stably, so that an expert's rows are in the order of the tokens: counts of each expert for each run of tokens, a
 // sum over the runs in front and the experts in front, and the rank within the run.  No atomic's order reaches a result.
 //
-// What bounds it: for few tokens the launches (1 token of 64 experts 2.8 us), for many the vector unit, some 40 instructions to a token's expert where scores are compared (16384 tokens of 512 experts in groups 52 us, their
+// What bounds it: for few tokens the launches (1 token of 64 experts 2.8 us), for many the vector unit, some 40 instructions to a token's expert where scores are compared (16384 tokens of 512 experts in groups 51 us, their
 // logits at 6.4 TB/s 5), some 10 where logits are (16384 of 128 7.8 us); the second launch reads all counts in every workgroup (6.5 us).
 #include "bf16_rows.hpp"
 #include "internal.hpp"
@@ -24,10 +24,9 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kMaxThreads = 1024, kMaxWaves = kMaxThreads / 64;
+// Threads of a workgroup at most that routes tokens: exact scores of sixteen experts to a lane take more registers than 1024 threads have.
+constexpr int threads_of(int lanes, int each) { return lanes * each > 512 ? 512 : kMaxThreads; }
 constexpr int kMaxRuns = 256;          // runs of tokens: a compute unit each, and few enough that every workgroup that places rows can read all counts
-
-// Threads of a workgroup at most that routes tokens: sixteen experts to a lane take more registers than 1024 threads have.
-constexpr int threads_of(int each) { return each > 8 ? 512 : kMaxThreads; }
 
 struct RouteArgs {
     const void* logits;
@@ -43,6 +42,7 @@ struct RouteArgs {
     int32_t* places;
     int32_t* counts;           // [runs, wide]
     int run, runs, wide;       // tokens of a run; runs; experts rounded up to a multiple of four
+    int words;                 // a power of two, for a bit to each token of a run
     bool sigmoid, renorm, sum2, alone;
     FastDiv by_size, by_top, by_fours;         // by the experts of a group, ..., a quarter of `wide`
 };
@@ -271,51 +271,76 @@ __device__ __forceinline__ bool any_lane(bool v)
     return lanes_max<LANES>((uint32_t)v) != 0;
 }
 
-// The choice by exact scores, by a whole wave with the keys in LDS: for tokens whose scores fp32 cannot tell apart.  Lane j is left the j-th expert, or -1.
-template <bool F32>
-__device__ __forceinline__ int choose_exactly(const RouteArgs& a, int64_t at, float most, u64* keys)
+// What leaves of a token: lane j has its j-th expert (or -1), and that one's logit.  Of a workgroup alone the experts are left in `count` too, else counted there.
+template <int LANES, bool F32>
+__device__ __forceinline__ void finish_token(const RouteArgs& a, const Token<LANES, F32>& k, int64_t t, bool real, bool bad, int mine, float of_mine, int32_t* count)
 {
-    constexpr int LANES = 64;
-    const int lane = threadIdx.x & 63;
-    Token<LANES, F32> k{a, lane, at, most, 1.0};
-    if (!a.sigmoid) {
-        double sum = 0.0;
-        for (int e = lane; e < a.experts; e += LANES) sum += k.exact_power(k.logit(e));
-        k.sum = lanes_sum<LANES>(sum);
+    float w = mine >= 0 ? k.weight(of_mine) : 0.0f;
+    const float whole = fmaxf((float)k.sum, 0x1p-60f);        // (of softmax w is e^(z - max): `whole` times the score)
+    if (a.renorm) w /= fmaxf(over_lanes<LANES>(w, [](float x, float y) { return x + y; }), 0x1p-60f * whole);
+    else w /= whole;
+    if (real && k.lane < a.top) {
+        a.weights[t * a.top + k.lane] = bad ? __builtin_nanf("") : w * a.scale;
+        a.chosen[t * a.top + k.lane] = mine;
+        if (a.alone) count[t * a.top + k.lane] = mine;
+        else if (mine >= 0) atomicAdd(count + mine, 1);
     }
-    for (int e = lane; e < a.experts; e += LANES) {
-        const float z = k.logit(e), b = a.bias ? a.bias[e] : 0.0f;
+}
+
+// A token whose scores fp32 cannot tell apart, by exact scores and by a whole wave; expert 64 i + lane is the lane's i-th.  keys: room in LDS for them.
+template <int EACH, bool F32>
+__device__ __forceinline__ void route_exactly(const RouteArgs& a, int64_t t, u64* keys, int32_t* count)
+{
+    Token<64, F32> k{a, (int)threadIdx.x & 63, t * a.stride, -__builtin_inff(), 1.0};
+    const int lane = k.lane;
+    // (four experts' exponentials at a time, each a long chain of its own)
+    auto logit = [&](int i) { return 64 * i + lane < a.experts ? k.logit(min(64 * i + lane, a.experts - 1)) : -__builtin_inff(); };
+    if (!a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) k.most = fmaxf(k.most, logit(i));
+        k.most = of_order(lanes_max<64>(order_of(k.most)));
+        double sum = 0.0;
+#pragma unroll 4
+        for (int i = 0; i < EACH; ++i) sum += k.exact_power(logit(i));
+        k.sum = lanes_sum<64>(sum);
+    }
+#pragma unroll 4
+    for (int i = 0; i < EACH; ++i) {
+        const int e = 64 * i + lane;
+        const float z = logit(i), b = a.bias ? a.bias[min(e, a.experts - 1)] : 0.0f;
         keys[e] = z == -__builtin_inff() || b == -__builtin_inff() ? 0 : order_of(k.exact_score(z) + (double)b);
     }
     __builtin_amdgcn_wave_barrier();
     u64 kept = ~0ull;
     bool sure = true;
-    if (a.groups > 1) kept = best_groups<LANES, true>(a, lane, 0.0f, sure, [&](int e) { return keys[e]; });
+    if (a.groups > 1) kept = best_groups<64, true>(a, lane, 0.0f, sure, [&](int e) { return keys[e]; });
+    u64 key[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) key[i] = kept >> (fast_div(min(64 * i + lane, a.experts - 1), a.by_size) & 63) & 1 ? keys[64 * i + lane] : 0;
     int mine = -1;
     for (int j = 0; j < a.top; ++j) {
         u64 best = 0;
         uint32_t e = 0xffffffffu;
-        for (int x = lane; x < a.experts; x += LANES) {
-            const u64 v = kept >> (fast_div(x, a.by_size) & 63) & 1 ? keys[x] : 0;
-            e = v > best ? x : e;
-            best = v > best ? v : best;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            e = key[i] > best ? 64 * i + lane : e;
+            best = key[i] > best ? key[i] : best;
         }
         const u64 of_lane = best;
-        best = lanes_max<LANES>(best);
-        if (!__any(best != 0)) break;
-        e = expert_of<LANES>(of_lane, best, e);
-        if (best != 0) {
-            if (lane == (int)(e & (LANES - 1))) keys[e] = 0;
-            if (lane == j) mine = (int)e;
-        }
-        __builtin_amdgcn_wave_barrier();
+        best = lanes_max<64>(best);
+        if (best == 0) break;
+        e = expert_of<64>(of_lane, best, e);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) key[i] = 64 * i + lane == (int)e ? 0 : key[i];
+        if (lane == j) mine = (int)e;
     }
-    return mine;
+    __builtin_amdgcn_wave_barrier();
+    finish_token<64, F32>(a, k, t, true, false, mine, mine >= 0 ? k.logit(mine) : 0.0f, count);
 }
 
-// The choice of a token to each LANES lanes; expert LANES i + lane is the lane's i-th.  keys: room in LDS for the token's keys.  Chosen experts are left in a.chosen, and counted; of a workgroup alone they are left in `count` too.
+// The choice of a token to each LANES lanes; expert LANES i + lane is the lane's i-th.  keys: room in LDS for the token's keys.  False where fp32 leaves it in doubt: then nothing was written.
 template <int LANES, int EACH, int BY, bool F32>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool real, u64* keys, int32_t* count)
+__device__ __forceinline__ bool route_token(const RouteArgs& a, int64_t t, bool real, u64* keys, int32_t* count)
 {
     Token<LANES, F32> k{a, (int)threadIdx.x & (LANES - 1), real ? t * a.stride : 0, 0.0f, 1.0};
     const int lane = k.lane;
@@ -421,28 +446,11 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool 
         for (int i = 0; i < EACH; ++i) next = max(next, key[i]);
         next = lanes_max<LANES>(next);
         sure &= next == 0 || apart(before, of_order(next), doubt);
-        for (u64 unsure = __ballot(real && !sure && lane == 0); unsure; unsure &= unsure - 1) {      // (a token that is bad has no keys, of which it is sure)
-            const int of = __builtin_ctzll(unsure), wave_lane = (int)threadIdx.x & 63;
-            const int64_t at = (int64_t)((u64)(uint32_t)__builtin_amdgcn_readlane((int)(k.at >> 32), of) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k.at, of));
-            const int exact = choose_exactly<F32>(a, at, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k.most), of)), keys - (wave_lane - lane) * EACH);
-            const int j = __builtin_amdgcn_ds_bpermute(lane * 4, exact);
-            if (wave_lane - lane == of) mine = j;
-            __builtin_amdgcn_wave_barrier();
-        }
         of_mine = mine >= 0 ? k.logit(mine) : 0.0f;
     }
 
-    // ---- weights
-    float w = mine >= 0 ? k.weight(of_mine) : 0.0f;
-    const float whole = fmaxf((float)k.sum, 0x1p-60f);        // (of softmax w is e^(z - max): `whole` times the score)
-    if (a.renorm) w /= fmaxf(over_lanes<LANES>(w, [](float x, float y) { return x + y; }), 0x1p-60f * whole);
-    else w /= whole;
-    if (real && lane < a.top) {
-        a.weights[t * a.top + lane] = bad ? __builtin_nanf("") : w * a.scale;
-        a.chosen[t * a.top + lane] = mine;
-        if (a.alone) count[t * a.top + lane] = mine;
-        else if (mine >= 0) atomicAdd(count + mine, 1);
-    }
+    finish_token<LANES, F32>(a, k, t, real && (BY != kScore || sure), bad, mine, of_mine, count);
+    return sure;
 }
 
 // Exclusive sum over a workgroup of kMaxThreads of one number a thread, and the whole.  part: [kMaxWaves] words of LDS.
@@ -500,19 +508,31 @@ __device__ __forceinline__ void place_few(const RouteArgs& a, const int32_t* kep
 // A run of tokens to a workgroup.  Where it is alone, it places the rows too (1 token x 4 of 64 experts 3.5 us, in two launches 6.1; 32 tokens 6.8 and 7.0; 64 tokens x 2 7.2 and 6.9, of which the host
 // has one less to make).
 template <int LANES, int EACH, int BY, bool F32>
-__global__ __launch_bounds__(threads_of(EACH)) void moe_route_kernel(RouteArgs a)
+__global__ __launch_bounds__(threads_of(LANES, EACH)) void moe_route_kernel(RouteArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int threads = blockDim.x, at_once = threads / LANES;
     int32_t* const count = reinterpret_cast<int32_t*>(smem);                // [experts], or alone the experts that were chosen [tokens, top]
     const int n = a.alone ? (int)a.tokens * a.top : a.experts;
-    u64* const keys = reinterpret_cast<u64*>(smem + (n + 3) / 4 * 16);      // of each token at a time, where they are needed
+    uint32_t* const doubtful = reinterpret_cast<uint32_t*>(smem + (n + 3) / 4 * 16);          // a bit to each token: the i-th in word i % words, so that they are spread over the waves
+    u64* const keys = reinterpret_cast<u64*>(smem + (n + 3) / 4 * 16 + (BY == kScore ? a.words * 4 : 0));      // of each token at a time, where they are needed
     for (int i = threadIdx.x; i < (n + 3) / 4 * 4; i += threads) count[i] = a.alone ? -1 : 0;
+    if constexpr (BY == kScore)
+        for (int i = threadIdx.x; i < a.words; i += threads) doubtful[i] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * a.run, end = min(first + a.run, a.tokens);
     for (int64_t t0 = first; t0 < end; t0 += at_once) {
         const int64_t t = t0 + threadIdx.x / LANES;
-        if (__any(t < end)) route_token<LANES, EACH, BY, F32>(a, t, t < end, keys + threadIdx.x / LANES * (LANES * EACH), count);
+        if (!__any(t < end)) continue;
+        const bool sure = route_token<LANES, EACH, BY, F32>(a, t, t < end, keys + threadIdx.x / LANES * (LANES * EACH), count);
+        if (BY == kScore && !sure && t < end && threadIdx.x % LANES == 0) atomicOr(doubtful + ((int)(t - first) & (a.words - 1)), 1u << (int)(t - first) / a.words);
+    }
+    if constexpr (BY == kScore) {      // (apart from the others, which have the registers for themselves then: 16384 tokens, 8 of 256 experts 32.3 -> 28.4 us in both launches, in groups 41.5 -> 35.1; without any in doubt 24.0 and 29.3)
+        __syncthreads();
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        for (int w = wave; w < a.words; w += threads / 64)
+            for (uint32_t bits = __builtin_amdgcn_readfirstlane(doubtful[w]); bits; bits &= bits - 1)
+                route_exactly<(LANES * EACH + 63) / 64, F32>(a, first + __builtin_ctz(bits) * a.words + w, keys + wave * (64 * EACH), count);
     }
     __syncthreads();
     if (a.alone) {
@@ -731,8 +751,8 @@ hipError_t route(const RouteArgs& a, hipStream_t st)
 {
     // (alone: enough to place the rows too, at a time)
     const int64_t wanted = std::max<int64_t>(std::min<int64_t>(a.run, a.tokens) * LANES, a.alone ? a.tokens * a.top + a.experts + 1 : 1);
-    const int waves = (int)std::min<int64_t>((wanted + 63) / 64, threads_of(EACH) / 64);
-    const size_t lds = (size_t)((a.alone ? a.tokens * a.top : a.experts) + 3) / 4 * 16 + (BY == kScore || a.groups > 1 ? (size_t)waves * 64 * EACH * 8 : 0);
+    const int waves = (int)std::min<int64_t>((wanted + 63) / 64, threads_of(LANES, EACH) / 64);
+    const size_t lds = (size_t)((a.alone ? a.tokens * a.top : a.experts) + 3) / 4 * 16 + (BY == kScore ? a.words * 4 : 0) + (BY == kScore || a.groups > 1 ? (size_t)waves * 64 * EACH * 8 : 0);
     static LdsAttrOnce attr;
     if (const hipError_t e = attr.ensure(reinterpret_cast<const void*>(moe_route_kernel<LANES, EACH, BY, F32>), 163840)) return e;
     hipLaunchKernelGGL((moe_route_kernel<LANES, EACH, BY, F32>), dim3(std::max(a.runs, 1)), dim3(waves * 64), lds, st, a);
@@ -770,7 +790,7 @@ size_t moe_count_bytes(int64_t tokens, int64_t experts, int64_t top)
 hipError_t launch_moe_route(const void* logits, int64_t stride, bool f32, const float* bias, int64_t tokens, int64_t experts, int64_t top, int64_t groups, int64_t top_groups, float scale,
                             bool sigmoid, bool renorm, bool sum2, float* weights, int32_t* chosen, int32_t* offsets, int32_t* rows, int32_t* places, void* counts, hipStream_t st)
 {
-    RouteArgs a{logits, stride, bias, tokens, (int)experts, (int)top, (int)groups, (int)top_groups, scale, weights, chosen, offsets, rows, places, static_cast<int32_t*>(counts), 0, 0, 0,
+    RouteArgs a{logits, stride, bias, tokens, (int)experts, (int)top, (int)groups, (int)top_groups, scale, weights, chosen, offsets, rows, places, static_cast<int32_t*>(counts), 0, 0, 0, kMaxWaves,
                 sigmoid, renorm, sum2 && groups > 1, alone(tokens, top), fast_div_by((uint32_t)(experts / groups)), fast_div_by((uint32_t)top), fast_div_by((uint32_t)(experts + 3) / 4)};
     runs_of(tokens, a.run, a.runs);
     a.wide = (int)(experts + 3) / 4 * 4;
@@ -778,6 +798,7 @@ hipError_t launch_moe_route(const void* logits, int64_t stride, bool f32, const 
         a.run = (int)tokens;
         a.runs = 1;
     }
+    while (a.words * 32 < a.run) a.words *= 2;
     hipError_t e;
     if (bias || a.sum2) e = f32 ? route<kScore, true>(a, st) : route<kScore, false>(a, st);
     else e = f32 ? route<kLogit, true>(a, st) : route<kPacked, false>(a, st);
