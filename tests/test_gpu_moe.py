@@ -157,6 +157,26 @@ def test_many_tokens(fp4, T):
         assert torch.equal(places.reshape(-1).long(), want)
 
 
+@pytest.mark.parametrize("T,E,top", [(40, 24, 3), (9000, 24, 3), (200003, 24, 3), (70001, 300, 2)])
+def test_every_token_in_doubt(fp4, T, E, top):
+    """Few different logits and biases: whatever the arithmetic, equal scores are equal, and every token's choice is among them.  Runs of tokens from a few to more than a bit to each of sixteen words holds."""
+    say(f"route in doubt T={T} E={E}")
+    g = torch.Generator().manual_seed(T)
+    z = (torch.randint(0, 4, (T, E), generator=g).float() * 0.5).cuda()
+    bias = (torch.arange(E) % 3 * 0.125).cuda()
+    for flags in (fp4.ROUTE_SIGMOID, 0):
+        weights, experts, rows, offsets, places = fp4.moe_route(z, top, bias=bias, flags=flags)
+        s = 1 / (1 + torch.exp(-z.double())) if flags else z.double().softmax(1)
+        # (softmax: sums of the same terms in other orders differ between rows, not within one: a row's equal logits have equal scores)
+        chosen = (s + bias.double()).sort(dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(experts, chosen.to(torch.int32))
+        assert ((weights - s.gather(1, chosen)).abs() <= s.gather(1, chosen) * 2.0 ** -20).all()
+        flat = chosen.reshape(-1)
+        order = torch.argsort(flat, stable=True)
+        assert torch.equal(rows, (order // top).to(torch.int32))
+        assert torch.equal(offsets.long(), torch.searchsorted(flat[order], torch.arange(E + 1, device="cuda")))
+
+
 def test_no_tokens(fp4):
     weights, experts, rows, offsets, places = fp4.moe_route(torch.empty(0, 37, device="cuda"), 4)
     assert weights.shape == experts.shape == places.shape == (0, 4) and rows.numel() == 0 and offsets.shape == (38,) and (offsets == 0).all()
