@@ -671,21 +671,25 @@ static_assert(Tile64::S <= kMostStages && Tile128n::S <= kMostStages && Tile128:
 constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 128, 128, 256}, kCols[kKinds] = {16, 32, 16, 32, 64, 64, 128, 256, 256};
 
 // What a kind takes, microseconds on a device of `cus` compute units, as fitted to measurements on 256: a start, rounds of tiles, each a fixed part and the steps of K (a quarter of its blocks where four waves share
-// them), but no less than what it reads takes from memory at `rate` TB/s: the weights, once for every row of tiles where rows are few, else both operands once, of the `sets` of weights that have rows.  Parts add the writing,
-// reading and launch of their sum.
-// Measured, each kind and number of parts forced in turn, on 336 products of 1 to 4096 rows with layers from 300 x 9600 to 28672 x 4096 and on 150 drawn ones: the kind that is chosen takes 1.015 of the best one's time in
-// the mean, at worst 1.34 (10 x 9714 x 8400: 21.6 us with tiles of 16 x 32, 16.1 on tiles of 64 x 64); the others up to ten times it (1 x 4096 x 4096: 16 x 16 5.6 us, 64 x 64 9.0, 128 x 128 15; 201 x 10240 x 8192: 128 x 128 27 us,
-// 128 x 64 37, 64 x 64 41, 128 x 256 50; 4096 x 4096 x 4096: 256 x 256 53 us, 128 x 256 63, 128 x 128 65, 64 x 64 100).
-double kind_us(int kind, double rows, double tiles_m, double sets, double N, double K, int64_t blocks, int parts, int cus)
+// them), but no less than what it reads takes from memory at `rate` TB/s: where rows are few the weights, once for the first row of tiles and `again` times for each other one (the caches have part of them), else both
+// operands once, of the `sets` of weights that have rows.  Parts add the writing, reading and launch of their sum.  A product by expert runs longer and is nearer to what memory gives: it has numbers of its own.
+// Measured, each kind and number of parts forced in turn, on 336 products of 1 to 4096 rows with layers from 300 x 9600 to 28672 x 4096 and on 150 drawn ones, weights from memory (450 MB of them in turn): the kind that is
+// chosen takes 1.015 of the best one's time in the mean, 1.017 on 100 others, at worst 1.26 (16 x 5001 x 2896: 8.1 us on tiles of 16 x 32, 6.4 on 16 x 16); by expert 1.04 on 66 products; the others up to ten times it
+// (1 x 4096 x 4096: 16 x 16 5.9 us, 64 x 64 9.9, 128 x 128 19; 16 x 10240 x 8192: 64 x 64 20.3, 16 x 16 25.6; 128 x 4096 x 14336: 128 x 64 in four parts 23, in one 50; 201 x 10240 x 8192: 128 x 128 27 us, 128 x 64 37,
+// 64 x 64 41, 128 x 256 50; 4096 x 4096 x 4096: 256 x 256 53 us, 128 x 256 63, 128 x 128 65, 64 x 64 100).
+double kind_us(int kind, bool grouped, double rows, double tiles_m, double sets, double N, double K, int64_t blocks, int parts, int cus)
 {
-    static const double start[] = {3.00, 3.16, 2.85, 3.03, 2.71, 2.56, 2.56, 2.54, 1.50}, fixed[] = {0.65, 0.42, 0.56, 0.78, 1.18, 1.74, 2.23, 3.00, 5.90},
-                        step[] = {0.129, 0.350, 0.284, 0.328, 0.183, 0.263, 0.406, 0.854, 1.254}, rate[] = {5.9, 7.35, 6.6, 5.8, 5.9, 6.1, 5.8, 4.1, 3.9};
-    static const int per_cu[] = {2, 3, 1, 1, 1, 1, 1, 1, 1};
+    static const double start[2][kKinds] = {{2.68, 2.94, 2.52, 2.66, 2.45, 3.04, 3.21, 3.88, 1.00}, {3.00, 3.16, 2.85, 3.03, 2.71, 2.56, 2.56, 2.54, 1.50}},
+                        fixed[2][kKinds] = {{0.61, 0.02, 0.56, 0.75, 0.92, 1.11, 1.54, 2.05, 6.20}, {0.65, 0.42, 0.56, 0.78, 1.18, 1.74, 2.23, 3.00, 5.90}},
+                        step[2][kKinds] = {{0.243, 0.486, 0.388, 0.557, 0.251, 0.344, 0.520, 1.007, 1.417}, {0.129, 0.350, 0.284, 0.328, 0.183, 0.263, 0.406, 0.854, 1.254}},
+                        rate[2][kKinds] = {{3.91, 3.87, 3.98, 4.08, 4.59, 4.23, 4.34, 10.6, 8.7}, {5.9, 7.35, 6.6, 5.8, 5.9, 6.1, 5.8, 4.1, 3.9}}, again[kFew] = {0.57, 0.23, 0.45, 0.07};
+    static const int per_cu[kKinds] = {2, 3, 1, 1, 1, 1, 1, 1, 1};
     const bool few = kind < kFew;
     const double steps = (double)(few ? (blocks + 3) / 4 : std::max<int64_t>((blocks + parts - 1) / parts, kStages[kind]));
-    const double rounds = std::ceil(tiles_m * std::ceil(N / kCols[kind]) * parts / (per_cu[kind] * cus)), bytes = few ? tiles_m * N * K : sets * N * K + rows * K;
-    const double us = start[kind] + std::max(rounds * (fixed[kind] + steps * step[kind]), bytes / (rate[kind] * 1e6 * cus / 256));
-    return parts > 1 ? us + 4.2 + parts * rows * N * 8 / 6.4e6 : us;
+    const double rounds = std::ceil(tiles_m * std::ceil(N / kCols[kind]) * parts / (per_cu[kind] * cus));
+    const double bytes = few ? (sets + (grouped ? 1.0 : again[kind]) * (tiles_m - sets)) * N * K : sets * N * K + rows * K;
+    const double us = start[grouped][kind] + std::max(rounds * (fixed[grouped][kind] + steps * step[grouped][kind]), bytes / (rate[grouped][kind] * 1e6 * cus / 256));
+    return parts > 1 ? us + 4.6 + parts * rows * N * 8 / 7.4e6 : us;
 }
 
 // The kind that takes least; in parts only where `room` bytes hold their sums and fewer would leave compute units idle.
@@ -706,7 +710,7 @@ Plan plan_int8(const Int8Args& g, bool grouped, size_t room)
             if (parts > 1 && (grouped || kind < kFew || kind > kFew + 2 || (size_t)parts * g.rows * g.N * 4 > room || (parts - 1) * each >= blocks)) break;
             if (parts > 1 && !forced && (parts - 1) * tiles >= cus) break;
             if (forced && parts > 1 << (forced - 1) / kKinds) break;
-            const double us = forced ? (double)-parts : kind_us(kind, (double)g.rows, tiles_m, grouped ? active : 1.0, (double)g.N, (double)g.K, blocks, parts, cus);
+            const double us = forced ? (double)-parts : kind_us(kind, grouped, (double)g.rows, tiles_m, grouped ? active : 1.0, (double)g.N, (double)g.K, blocks, parts, cus);
             if (us < best_us) {
                 best = Plan{kind, parts, (int)each};
                 best_us = us;
