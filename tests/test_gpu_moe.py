@@ -177,6 +177,27 @@ def test_every_token_in_doubt(fp4, T, E, top):
         assert torch.equal(offsets.long(), torch.searchsorted(flat[order], torch.arange(E + 1, device="cuda")))
 
 
+def test_as_many_tokens_as_there_may_be(fp4):
+    say("route T=2^24")
+    T, E, top = 1 << 24, 8, 2
+    z = torch.randn(T, E, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(torch.bfloat16)
+    bias = (0.1 * torch.arange(E)).cuda()
+    weights, experts, rows, offsets, places = fp4.moe_route(z, top, bias=bias, flags=fp4.ROUTE_SIGMOID)
+    # (of two equal scores the lower index: eight experts in descending order of their score, chosen one by one)
+    c = 1 / (1 + torch.exp(-z.double())) + bias.double()
+    first = c.argmax(1)
+    first = (c == c.gather(1, first[:, None])).float().argmax(1)
+    c.scatter_(1, first[:, None], -1.0)
+    second = (c == c.max(1, keepdim=True).values).float().argmax(1)
+    assert torch.equal(experts[:, 0].long(), first) and torch.equal(experts[:, 1].long(), second)
+    del c
+    assert torch.equal(offsets[1:].long(), torch.bincount(experts.reshape(-1).long(), minlength=E).cumsum(0))
+    flat = experts.reshape(-1)
+    order = torch.argsort(flat, stable=True)
+    assert torch.equal(rows.long(), order // top)
+    assert torch.equal(places.reshape(-1)[order], torch.arange(T * top, device="cuda", dtype=torch.int32))
+
+
 def test_no_tokens(fp4):
     weights, experts, rows, offsets, places = fp4.moe_route(torch.empty(0, 37, device="cuda"), 4)
     assert weights.shape == experts.shape == places.shape == (0, 4) and rows.numel() == 0 and offsets.shape == (38,) and (offsets == 0).all()
