@@ -38,24 +38,18 @@ __device__ __forceinline__ v4i mfma(const v4i& a, const v4i& b, const v4i& c) { 
 template <int OUT>
 __device__ __forceinline__ void store4(void* out, int64_t at, const v4i& sum, float sa, const v4f& sw, int have)
 {
-    if constexpr (OUT == kSums) {
-        int* const to = static_cast<int*>(out) + at;
-        if (have >= 4) __builtin_memcpy(to, &sum, 16);
-        else for (int e = 0; e < have; ++e) to[e] = sum[e];
-    } else {
-        float y[4];
+    float y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (float)sum[e] * sa * sw[e];
-        if constexpr (OUT == kF32) {
-            float* const to = static_cast<float*>(out) + at;
-            if (have >= 4) __builtin_memcpy(to, y, 16);
-            else for (int e = 0; e < have; ++e) to[e] = e == 0 ? y[0] : e == 1 ? y[1] : y[2];
-        } else {
-            const __bf16 b[4] = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-            __bf16* const to = static_cast<__bf16*>(out) + at;
-            if (have >= 4) __builtin_memcpy(to, b, 8);
-            else for (int e = 0; e < have; ++e) to[e] = e == 0 ? b[0] : e == 1 ? b[1] : b[2];
-        }
+    for (int e = 0; e < 4; ++e) y[e] = (float)sum[e] * sa * sw[e];
+    if constexpr (OUT == kF32) {
+        float* const to = static_cast<float*>(out) + at;
+        if (have >= 4) __builtin_memcpy(to, y, 16);
+        else for (int e = 0; e < have; ++e) to[e] = e == 0 ? y[0] : e == 1 ? y[1] : y[2];
+    } else {
+        const __bf16 b[4] = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+        __bf16* const to = static_cast<__bf16*>(out) + at;
+        if (have >= 4) __builtin_memcpy(to, b, 8);
+        else for (int e = 0; e < have; ++e) to[e] = e == 0 ? b[0] : e == 1 ? b[1] : b[2];
     }
 }
 
@@ -125,11 +119,9 @@ __global__ __launch_bounds__(C::WAVES * 64) void int8_stream_kernel(Int8Args g, 
         }
         const int w_rows = min((int)g.N - n0, 16 * TN);
         rw = make_rsrc(g.w + ((int64_t)r.expert * g.N + n0) * K, (int64_t)w_rows * K);
-        if constexpr (OUT != kSums) {
-            const int to = C::kScales + (tile & 7) * C::SCALES;
-            if (wave == 0) load_lds4(make_rsrc(g.a_scales + x0, x_rows * 4), smem, to, x_offset(min(lane, 16 * TM - 1), 4));
-            if (wave == 1) load_lds4(make_rsrc(g.w_scales + (int64_t)r.expert * g.N + n0, w_rows * 4), smem, to + 256, (uint32_t)min(lane, 16 * TN - 1) * 4);
-        }
+        const int to = C::kScales + (tile & 7) * C::SCALES;
+        if (wave == 0) load_lds4(make_rsrc(g.a_scales + x0, x_rows * 4), smem, to, x_offset(min(lane, 16 * TM - 1), 4));
+        if (wave == 1) load_lds4(make_rsrc(g.w_scales + (int64_t)r.expert * g.N + n0, w_rows * 4), smem, to + 256, (uint32_t)min(lane, 16 * TN - 1) * 4);
     };
     int load_tile = tile_first, load_kb = 0, load_slot = 0;
     auto issue = [&]() {
