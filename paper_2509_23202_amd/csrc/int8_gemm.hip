@@ -666,15 +666,15 @@ constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 128, 128, 256}, kCols[kK
 // them), but no less than what it reads takes from memory at `rate` TB/s: where rows are few the weights, once for the first row of tiles and `again` times for each other one (the caches have part of them), else both
 // operands once, of the `sets` of weights that have rows.  Parts add the writing, reading and launch of their sum.  A product by expert runs longer and is nearer to what memory gives: it has numbers of its own.
 // Measured, each kind and number of parts forced in turn, on 336 products of 1 to 4096 rows with layers from 300 x 9600 to 28672 x 4096 and on 150 drawn ones, weights from memory (450 MB of them in turn): the kind that is
-// chosen takes 1.015 of the best one's time in the mean, 1.017 on 100 others, at worst 1.26 (16 x 5001 x 2896: 8.1 us on tiles of 16 x 32, 6.4 on 16 x 16); by expert 1.04 on 66 products; the others up to ten times it
+// chosen takes 1.017 of the best one's time in the mean, 1.017 on 100 others too, at worst 1.26 (16 x 5001 x 2896: 8.1 us on tiles of 16 x 32, 6.4 on 16 x 16); by expert 1.04 on 66 products; the others up to ten times it
 // (1 x 4096 x 4096: 16 x 16 5.9 us, 64 x 64 9.9, 128 x 128 19; 16 x 10240 x 8192: 64 x 64 20.3, 16 x 16 25.6; 128 x 4096 x 14336: 128 x 64 in four parts 23, in one 50; 201 x 10240 x 8192: 128 x 128 27 us, 128 x 64 37,
 // 64 x 64 41, 128 x 256 50; 4096 x 4096 x 4096: 256 x 256 53 us, 128 x 256 63, 128 x 128 65, 64 x 64 100).
 double kind_us(int kind, bool grouped, double rows, double tiles_m, double sets, double N, double K, int64_t blocks, int parts, int cus)
 {
-    static const double start[2][kKinds] = {{2.68, 2.94, 2.52, 2.66, 2.45, 3.04, 3.21, 3.88, 1.00}, {3.00, 3.16, 2.85, 3.03, 2.71, 2.56, 2.56, 2.54, 1.50}},
-                        fixed[2][kKinds] = {{0.61, 0.02, 0.56, 0.75, 0.92, 1.11, 1.54, 2.05, 6.20}, {0.65, 0.42, 0.56, 0.78, 1.18, 1.74, 2.23, 3.00, 5.90}},
-                        step[2][kKinds] = {{0.243, 0.486, 0.388, 0.557, 0.251, 0.344, 0.520, 1.007, 1.417}, {0.129, 0.350, 0.284, 0.328, 0.183, 0.263, 0.406, 0.854, 1.254}},
-                        rate[2][kKinds] = {{3.91, 3.87, 3.98, 4.08, 4.59, 4.23, 4.34, 10.6, 8.7}, {5.9, 7.35, 6.6, 5.8, 5.9, 6.1, 5.8, 4.1, 3.9}}, again[kFew] = {0.57, 0.23, 0.45, 0.07};
+    static const double start[2][kKinds] = {{2.68, 2.58, 2.52, 2.66, 2.45, 3.04, 3.21, 3.88, 1.00}, {3.00, 3.16, 2.85, 3.03, 2.71, 2.56, 2.56, 2.54, 1.50}},
+                        fixed[2][kKinds] = {{0.61, 0.42, 0.56, 0.75, 0.92, 1.11, 1.54, 2.05, 6.20}, {0.65, 0.42, 0.56, 0.78, 1.18, 1.74, 2.23, 3.00, 5.90}},
+                        step[2][kKinds] = {{0.243, 0.485, 0.388, 0.557, 0.251, 0.344, 0.520, 1.007, 1.417}, {0.129, 0.350, 0.284, 0.328, 0.183, 0.263, 0.406, 0.854, 1.254}},
+                        rate[2][kKinds] = {{3.91, 3.69, 3.98, 4.08, 4.59, 4.23, 4.34, 5.14, 3.40}, {5.9, 7.35, 6.6, 5.8, 5.9, 6.1, 5.8, 4.1, 3.9}}, again[kFew] = {0.57, 0.21, 0.45, 0.13};
     static const int per_cu[kKinds] = {2, 3, 1, 1, 1, 1, 1, 1, 1};
     const bool few = kind < kFew;
     const double steps = (double)(few ? (blocks + 3) / 4 : std::max<int64_t>((blocks + parts - 1) / parts, kStages[kind]));
