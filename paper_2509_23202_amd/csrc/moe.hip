@@ -142,9 +142,20 @@ __device__ __forceinline__ float power_of_e(float x, float lo = 0.0f)
 enum { kPacked, kLogit, kScore };
 
 // A score in fp32, from an exponential within two steps, sums in binary64 and a reciprocal, is within 2^-20 of the score: of softmax (x = z - max) s (2^-22 + 2^-22 + 2^-23 + 2^-24) + s 2^-24 sum e^x |x| / sum e^x
-// + 0.37 2^-24, where s times the quotient of sums is less than 2 (0.84 2^-20 in all), of sigmoid s (2^-22 + 2^-24 + 2^-23) + 0.28 2^-24.  With its bias it is within 2^-20 + 2^-24 (1 + |bias|), a sum of two of them
-// within twice 2^-20 + 2^-23 (1 + the largest |bias|), the doubt.  Two that are further apart than twice their doubt are in the order of their exact values.
-__device__ __forceinline__ bool apart(float larger, float smaller, float doubt) { return larger - smaller > 2.0f * doubt; }
+// + 0.37 2^-24, where s times the quotient of sums is less than 2 (0.84 2^-20 in all), of sigmoid s (2^-22 + 2^-24 + 2^-23) + 0.28 2^-24.  With its bias, c is within 2^-20 + 2^-24 |c|.
+// Two that are further apart than both errors, at most 2^-19 + 2^-23 of the larger magnitude, are in the order of their exact values; `apart` asks for twice the second part.  An error grows slower than c, so one that is
+// apart from the next is apart from all behind it; and it is a matter of the two that are compared: an expert that a bias far below the others takes out (-1e9, the type's lowest value) puts no token in
+// doubt (16384 tokens, 8 of 256 experts, one of which is out so: 27 us; with one doubt for all, from the largest bias, every token was routed twice: 53).
+__device__ __forceinline__ bool apart(float larger, float smaller) { return larger - smaller > fmaf(0x1p-22f, fmaxf(larger, -smaller), 0x1p-19f + 0x1p-22f); }
+
+// The same of sums m of two, f >= s: within 2^-19 + 2^-24 (|f| + |s| + |m|), at most 2^-19 + 2^-23 (|m| + opposed), the lesser magnitude of the two where their signs differ.  What is beyond fp32 counts as its largest
+// number, which the exact sum has passed but for a rounding.
+__device__ __forceinline__ bool sums_apart(float larger, float smaller, float opposed)
+{
+    constexpr float MOST = 3.402823466e38f;
+    const float l = __builtin_amdgcn_fmed3f(larger, -MOST, MOST), s = __builtin_amdgcn_fmed3f(smaller, -MOST, MOST);
+    return l - s > fmaf(0x1p-21f, fmaxf(l, -s) + opposed, 0x1p-18f + 0x1p-21f);
+}
 
 // A token's LANES lanes' view of what is the same for all of them.
 template <int LANES, bool F32>
@@ -173,13 +184,24 @@ struct Token {
     }
 };
 
-// The best top_groups groups, as bits.  key: a function of the expert.  sure: stays so where keys in fp32, each within `doubt`, leave none.
+// The wave's largest, and 1 at least: what hardly ever counts needs no maximum over the lanes.
+__device__ __forceinline__ float largest_opposed(float opposed)
+{
+    return __any(opposed > 1.0f) ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)lanes_max<64>(__float_as_uint(opposed)))) : 1.0f;
+}
+
+// The best top_groups groups, as bits.  key: a function of the expert.  sure: stays so where scores in fp32 leave no doubt.
 template <int LANES, bool EXACT, typename K>
-__device__ __forceinline__ u64 best_groups(const RouteArgs& a, int lane, float doubt, bool& sure, K key)
+__device__ __forceinline__ u64 best_groups(const RouteArgs& a, int lane, bool& sure, K key)
 {
     typedef std::conditional_t<EXACT, u64, uint32_t> Key;
     const int size = (int)a.by_size.d;
-    auto mark_of = [&](Key first, Key second) -> Key { return !a.sum2 || !second ? first : order_of(of_order(first) + of_order(second)); };
+    float opposed = 0.0f, of_wave = 0.0f;
+    auto mark_of = [&](Key first, Key second) -> Key {
+        if (!a.sum2 || !second) return first;
+        if constexpr (!EXACT) opposed = fmaxf(opposed, fminf(of_order(first), -of_order(second)));
+        return order_of(of_order(first) + of_order(second));
+    };
     auto add = [](Key k, Key& first, Key& second) {
         second = k > first ? first : k > second ? k : second;
         first = k > first ? k : first;
@@ -207,9 +229,10 @@ __device__ __forceinline__ u64 best_groups(const RouteArgs& a, int lane, float d
         }
         const bool own = (lane & (wide - 1)) == 0 && mark != 0;
         if constexpr (!EXACT) {      // the last one that is kept and the first that is not
+            of_wave = largest_opposed(opposed);
             const u64 last = __ballot(own && rank == a.top_groups - 1), out = __ballot(own && rank == a.top_groups);
             if (last && out)
-                sure &= apart(of_order((uint32_t)__builtin_amdgcn_readlane((int)mark, __builtin_ctzll(last))), of_order((uint32_t)__builtin_amdgcn_readlane((int)mark, __builtin_ctzll(out))), 2.0f * doubt);
+                sure &= sums_apart(of_order((uint32_t)__builtin_amdgcn_readlane((int)mark, __builtin_ctzll(last))), of_order((uint32_t)__builtin_amdgcn_readlane((int)mark, __builtin_ctzll(out))), of_wave);
         }
         u64 kept = 0;
         for (u64 of = __ballot(own && rank < a.top_groups); of; of &= of - 1) kept |= 1ull << __builtin_ctzll(of) / wide;
@@ -225,6 +248,8 @@ __device__ __forceinline__ u64 best_groups(const RouteArgs& a, int lane, float d
                 for (int j = 0; j < size; ++j) add(key(g * size + j), first, second);
             mark[q] = mark_of(first, second);
         }
+        if constexpr (!EXACT)
+            of_wave = largest_opposed(opposed);
         u64 kept = 0;
         Key last = 0;
         for (int j = 0; j <= a.top_groups; ++j) {
@@ -234,7 +259,7 @@ __device__ __forceinline__ u64 best_groups(const RouteArgs& a, int lane, float d
             best = lanes_max<LANES>(best);
             if (!__any(best != 0)) break;
             if (j == a.top_groups) {      // one that is left out
-                if constexpr (!EXACT) sure &= best == 0 || apart(of_order(last), of_order(best), 2.0f * doubt);
+                if constexpr (!EXACT) sure &= best == 0 || sums_apart(of_order(last), of_order(best), of_wave);
                 break;
             }
             uint32_t g = 64;
@@ -313,7 +338,7 @@ __device__ __forceinline__ void route_exactly(const RouteArgs& a, int64_t t, u64
     __builtin_amdgcn_wave_barrier();
     u64 kept = ~0ull;
     bool sure = true;
-    if (a.groups > 1) kept = best_groups<64, true>(a, lane, 0.0f, sure, [&](int e) { return keys[e]; });
+    if (a.groups > 1) kept = best_groups<64, true>(a, lane, sure, [&](int e) { return keys[e]; });
     u64 key[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) key[i] = kept >> (fast_div(min(64 * i + lane, a.experts - 1), a.by_size) & 63) & 1 ? keys[64 * i + lane] : 0;
@@ -386,19 +411,12 @@ __device__ __forceinline__ bool route_token(const RouteArgs& a, int64_t t, bool 
         }
     }
     bool sure = true;
-    float doubt = 0.0f;
-    if constexpr (BY == kScore) {
-        uint32_t largest = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) largest = max(largest, b[i] == -__builtin_inff() ? 0u : __float_as_uint(fabsf(b[i])));
-        doubt = 0x1p-20f + 0x1p-23f * (1.0f + __uint_as_float(lanes_max<LANES>(largest)));
-    }
     if (a.groups > 1) {
         uint32_t* const keys32 = reinterpret_cast<uint32_t*>(keys);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) keys32[LANES * i + lane] = BY == kPacked ? key[i] >> 16 : key[i];      // (equal groups: the lower one)
         __builtin_amdgcn_wave_barrier();
-        const u64 kept = best_groups<LANES, false>(a, lane, doubt, sure, [&](int e) { return keys32[e]; });
+        const u64 kept = best_groups<LANES, false>(a, lane, sure, [&](int e) { return keys32[e]; });
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
             if (!(kept >> fast_div(min(LANES * i + lane, a.experts - 1), a.by_size) & 1)) key[i] = 0;
@@ -407,7 +425,7 @@ __device__ __forceinline__ bool route_token(const RouteArgs& a, int64_t t, bool 
 
     // ---- the choice: lane j keeps the j-th, and its logit where the key has it
     int mine = -1;
-    float of_mine = 0.0f, before = __builtin_inff();
+    float of_mine = 0.0f, before = 3.402823466e38f;
     for (int j = 0; j < a.top; ++j) {
         uint32_t best = 0, e = 0xffffffffu;
         if constexpr (BY == kPacked) {
@@ -432,7 +450,7 @@ __device__ __forceinline__ bool route_token(const RouteArgs& a, int64_t t, bool 
         if (!__any(best != 0)) break;
         const float value = of_order(BY == kPacked ? (best & 0xffff0000u) | (best & 0x80000000u ? 0u : 0xffffu) : best);
         if (best != 0) {
-            if constexpr (BY == kScore) sure &= apart(before, value, doubt);
+            if constexpr (BY == kScore) sure &= apart(before, value);
             before = value;
             if (lane == j) {
                 mine = (int)e;
@@ -445,7 +463,7 @@ __device__ __forceinline__ bool route_token(const RouteArgs& a, int64_t t, bool 
 #pragma unroll
         for (int i = 0; i < EACH; ++i) next = max(next, key[i]);
         next = lanes_max<LANES>(next);
-        sure &= next == 0 || apart(before, of_order(next), doubt);
+        sure &= next == 0 || apart(before, of_order(next));
         of_mine = mine >= 0 ? k.logit(mine) : 0.0f;
     }
 
