@@ -439,7 +439,8 @@ fp4mr_status_t fp8_grouped_gemm(const void* a_codes, const float* a_scales, int6
  * channel of the weights (codes [N,K], scales [N]; of several experts [E,N,K] and [E,N]), all row-major and contiguous.  An operand stands for  code * scale.  The quantizers write
  *   scale = max(amax, 2^-100) / 127 ,  code = the integer nearest to  v * (127 * (1 / max(amax, 2^-100))) , ties to even ,
  * with amax the row's largest |v|, every operation in binary32 (of a bf16 tensor as it is, the code of the exact quotient 127 v / amax; one in the middle of two codes may be either); codes are -127 .. 127.  A row that holds a NaN or an infinity has
- * a scale that is not finite, and every output of a product that reads it is NaN or infinite.
+ * a scale that is not finite, and every output of a product that reads it is NaN or infinite.  The norm of a row of finite numbers is that of its definition whatever their size: squares beyond binary32, at either end,
+ * are formed of the row times a power of two.  A row of zeros with an eps of 0 has none (0 / 0) and a scale that is NaN.
  * K is a multiple of 16 in all calls and at most FP4MR_INT8_MAX_K (FP4MR_ERR_SHAPE), so that a sum of K products of any codes has 32 bits; M and N are any sizes; M, N <= 2^24 (M of int8_quantize 2^31), in products
  * M N <= 2^38.  No rows (M, or rows, of 0) is not an error: the call returns FP4MR_OK, launches nothing, and looks at no data pointer.  Scales, and the outputs of products, need the alignment of their
  * elements only.

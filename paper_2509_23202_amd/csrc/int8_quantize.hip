@@ -28,21 +28,6 @@ __device__ __forceinline__ v2i codes8(const float (&v)[8], float inv)
     return v2i{(int)(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24), (int)(b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24)};
 }
 
-// Largest of the workgroup's values, in all threads.  part: T / 64 words of LDS.
-template <int T>
-__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* part)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-    if constexpr (T > 64) {
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < T / 64; ++i) m = max(m, part[i]);
-    }
-    return m;
-}
-
 struct QuantArgs {
     const __bf16* x;
     int64_t x_stride, rows;
@@ -166,16 +151,7 @@ __global__ __launch_bounds__(T) void int8_rmsnorm_kernel(NormArgs a)
         for (int i = 0; i < 8; ++i) part_sum = fmaf(v[c][i], v[c][i], part_sum);
         sum += col < a.K ? part_sum : 0.0f;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if constexpr (T > 64) {
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < T / 64; ++i) sum += part[i];
-    }
-    const float rstd = 1.0f / sqrtf(sum / (float)a.K + a.eps);
+    const float rstd = row_factor<T, CH>(v, block_sum<T>(sum, part), a.K, a.eps);
     uint32_t m = 0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
