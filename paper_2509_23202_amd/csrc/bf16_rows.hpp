@@ -48,12 +48,21 @@ __device__ __forceinline__ float silu_mul(float g, float u)
     return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
 }
 
+// The lane's number, taken for another one at each use: what an exchange computes from it holds no registers until the next.
+__device__ __forceinline__ int own_lane()
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // Largest of the workgroup's values, in all threads.  part: T / 64 words of LDS.
 template <int T>
 __device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* part)
 {
+    const int lane = own_lane();
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__builtin_amdgcn_ds_bpermute((lane ^ d) << 2, (int)m));
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
         __syncthreads();
@@ -67,8 +76,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* part)
 template <int T>
 __device__ __forceinline__ float block_sum(float v, float* part)
 {
+    const int lane = own_lane();
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    for (int d = 1; d < 64; d <<= 1) v += __int_as_float(__builtin_amdgcn_ds_bpermute((lane ^ d) << 2, __float_as_int(v)));
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
         __syncthreads();
