@@ -385,6 +385,8 @@ fp4mr_status_t fp4_probe(int which, void* buf, size_t bytes, int iters, void* st
  *                where x_stride == K
  *   weight       bf16 [K];  K <= 65536
  *   norm_out     bf16 [M,K] or NULL: receives v rounded to bf16 (what a router reads)
+ * The norm of a row of finite numbers is that of this definition whatever their size: squares beyond binary32, at either end, are formed of the row times a power of two.  A row of
+ * zeros with an eps of 0 has none (0 / 0) and scales that are NaN.
  * Outputs must not overlap inputs or each other other than as said.  eps >= 0, else FP4MR_ERR_SHAPE.  A row's squares are added in an order that is
  * the same every time, but for 4096 < K <= 8192 another one in calls of more rows than there are compute units: last bits of v may then differ.
  */

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
 {
     __shared__ float part[T / 64];
     const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
     v4i x[CH], r[CH], w[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -119,16 +119,7 @@ __global__ __launch_bounds__(T) void fp8_rmsnorm_kernel(NormArgs a)
         for (int i = 0; i < 8; ++i) part_sum = fmaf(v[c][i], v[c][i], part_sum);
         sum += col < a.K ? part_sum : 0.0f;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if constexpr (T > 64) {
-        if (lane == 0) part[wave] = sum;
-        __syncthreads();
-        sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < T / 64; ++i) sum += part[i];
-    }
-    const float rstd = 1.0f / sqrtf(sum / (float)a.K + a.eps);
+    const float rstd = row_factor<T, CH>(v, block_sum<T>(sum, part), a.K, a.eps);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * T + (int)threadIdx.x) * 8;

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests import int8_util
+from tests import fp8_util, int8_util
 from tests.test_gpu_int8 import bf16, fp4, say  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,32 @@ def test_int8_rmsnorm_of_rows_that_are_not_finite_or_have_no_norm(fp4):
     bad[[0, 9, 4, 12]] = True
     assert not torch.isfinite(scales[bad]).any()
     assert torch.equal(codes[~bad], good[0][~bad]) and torch.equal(scales[~bad], good[1][~bad])
+
+
+@pytest.mark.parametrize("K", [128, 640, 1280, 2560, 4096, 8192, 8320, 16384, 32768, 40064, 65536])
+@pytest.mark.parametrize("eps", [0.0, 1e-38, 1e-30, 1e-6, 1e30])
+def test_fp8_rmsnorm_of_rows_whose_squares_are_beyond_binary32(fp4, K, eps):
+    say(f"fp8 rmsnorm K={K} eps={eps}")
+    x = rows_of_all_sizes(K, K)
+    w = (1.0 + 0.2 * torch.randn(K, generator=torch.Generator().manual_seed(9)).clamp(-3, 3)).to(torch.bfloat16).cuda()
+    delta = (0.5 * (64 + 21) + 9) * U        # as above
+    for residual, rows in ((None, 1), (torch.zeros_like(x), 1), (None, 20)):       # (rows of 8192 columns have other threads in calls of many rows)
+        h, n = x.repeat(rows, 1), torch.empty(rows * len(x), K, dtype=torch.bfloat16, device="cuda")
+        codes, scales, out = fp4.fp8_rmsnorm_quantize(h, w, eps, residual=residual, norm_out=n)
+        assert residual is None or torch.equal(out, x)
+        v = definition(x, w, eps)
+        fp8_util.check_operand(codes[-len(x):], scales[-len(x):], v, delta)
+        assert (np.abs(fp8_util.f64(n[-len(x):]) - v) <= np.abs(v) * (2.0 ** -8 + delta) + 2.0 ** -134).all()
+
+
+def test_fp8_rmsnorm_of_rows_that_are_not_finite_or_have_no_norm(fp4):
+    K = 1280
+    x = rows_of_all_sizes(K, 3)
+    w = torch.ones(K, dtype=torch.bfloat16, device="cuda")
+    good = fp4.fp8_rmsnorm_quantize(x, w, 0.0)
+    x[0, 5], x[9, 1270], x[4, 700], x[12] = float("inf"), float("nan"), -float("inf"), 0.0
+    codes, scales, _ = fp4.fp8_rmsnorm_quantize(x, w, 0.0)
+    bad = torch.zeros(len(x), dtype=torch.bool, device="cuda")
+    bad[[0, 9, 4, 12]] = True
+    assert not torch.isfinite(scales[bad]).all(1).any()
+    assert torch.equal(codes.view(torch.uint8)[~bad], good[0].view(torch.uint8)[~bad]) and torch.equal(scales[~bad], good[1][~bad])
