@@ -383,3 +383,24 @@ def test_two_streams_at_once_and_two_graphs(fp4):
                 g.replay()
         torch.cuda.synchronize()
         assert all(same(h, i) for i, h in enumerate(held))
+
+
+def test_combine_of_more_tokens_than_a_launch_has(fp4):
+    """Wide rows: a launch takes 2^22 tokens.  Places, weights, the shared expert's rows and the outputs of the next one begin there; the sums are those of the same tokens in calls of their own."""
+    say("combine of 2^22 + 600 tokens")
+    T, H, top, R_ = (1 << 22) + 600, 1032, 2, 999
+    g = torch.Generator(device="cuda").manual_seed(7)
+    y = torch.randn(R_, H, device="cuda", generator=g).to(torch.bfloat16)
+    places = torch.randint(-1, R_, (T, top), dtype=torch.int32, device="cuda", generator=g)
+    weights = torch.randn(T, top, device="cuda", generator=g)
+    shared = torch.empty(T, H, dtype=torch.bfloat16, device="cuda").random_(-100, 100, generator=g)
+    out = fp4.moe_combine(y, places, weights, shared=shared)
+    for at in range(0, T, 100000):
+        part = slice(at, min(at + 100000, T))
+        assert torch.equal(out[part], fp4.moe_combine(y, places[part], weights[part], shared=shared[part])), at
+    # the tokens on both sides by the definition: two products and two sums in fp32, one rounding
+    for part in (slice(0, 50), slice((1 << 22) - 50, (1 << 22) + 50), slice(T - 50, T)):
+        terms = torch.where((places[part] >= 0)[:, :, None], y[places[part].clamp(min=0).long()], y.new_zeros(1)).double() * weights[part].double()[:, :, None]
+        want, size = terms.sum(1) + shared[part].double(), terms.abs().sum(1) + shared[part].double().abs()
+        bound = size * 2 * 2.0 ** -24
+        assert ((out[part].double() - want).abs() <= bound + (want.abs() + bound) * 2.0 ** -8).all()
