@@ -458,3 +458,50 @@ def test_two_streams_at_once(fp4, M, N, parts):
                 got[i].append(fp4.int8_gemm(*fp4.int8_quantize(x), w, sw))
     torch.cuda.synchronize()
     assert all(torch.equal(g, want[i]) for i in range(2) for g in got[i])
+
+
+def test_parts_of_k_in_a_graph(fp4):
+    """The parts and the launch that joins them, recorded with a workspace of their own and replayed on other inputs, with eager work in the same form of room between the replays."""
+    M, N, K = 160, 4096, 14336
+    need = fp4.int8_workspace_bytes(M, N, K)
+    assert need > 0
+    xs = [bf16(M, K, 70 + i).contiguous() for i in range(3)]
+    w, sw = R.operand(N, K, 80, 0.01)
+    x, room = xs[0].clone(), torch.full((need,), 0x7f, dtype=torch.uint8, device="cuda")
+    want = []
+    for xi in xs:
+        (c, s), pick = fp4.int8_quantize(xi), torch.tensor([0, 77, 159], device="cuda")
+        want.append(fp4.int8_gemm(c, s, w, sw))
+        assert torch.equal(want[-1][pick].cpu(), R.product(c[pick], s[pick], w, sw, torch.bfloat16))
+    out = torch.zeros_like(want[0])
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            fp4.int8_gemm(*fp4.int8_quantize(x), w, sw, out=out, workspace=room)
+    for rnd in range(3):
+        for i, xi in enumerate(xs):
+            x.copy_(xi)
+            out.zero_()
+            room.fill_(0x55 + i)
+            assert torch.equal(fp4.int8_gemm(*fp4.int8_quantize(xi), w, sw), want[i])
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[i]), (rnd, i)
+
+
+def test_norm_of_a_prompt_repeats_itself_and_differs_from_64_bits_in_ties_alone(fp4):
+    """The residual's addition and the norm of 4095 x 8192, with loud channels: the same bits every time, and the code of the 64-bit quotient but where that is the middle of two within the roundings' reach."""
+    M, K = 4095, 8192
+    x, r = bf16(M, K, 90, loud=False), bf16(M, K, 91)
+    w = (1.0 + 0.2 * torch.randn(K, generator=torch.Generator().manual_seed(92))).to(torch.bfloat16).cuda()
+    first = fp4.int8_rmsnorm_quantize(x, w, 1e-6, residual=r)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(fp4.int8_rmsnorm_quantize(x, w, 1e-6, residual=r), first))
+    h = first[2].double()
+    assert torch.equal(first[2], (x.float() + r.float()).to(torch.bfloat16))
+    v = h / ((h * h).mean(1, keepdim=True) + 1e-6).sqrt() * w.double()
+    t = v * (127.0 / v.abs().amax(1, keepdim=True))
+    # The factor of the whole row is the same in v and in its largest: what is left are the two products of each, the reciprocal and the two products that make the code, seven roundings.
+    assert ((first[0].double() - t).abs() <= 0.5 + t.abs() * 7 * U).all()
