@@ -475,8 +475,9 @@ fp4mr_status_t int8_grouped_gemm(const void* a_codes, const float* a_scales, int
 /*
  * A router's choice: from the logits of T tokens to each one's `top` experts with their weights, and to the rows by expert that the grouped products take.
  *   s[t,e] = softmax over e of logits[t,:], or sigmoid(logits[t,e]) with FP4MR_ROUTE_SIGMOID;   c[t,e] = logits[t,e], or s[t,e] + bias[e] where there is a bias
- *   groups       the experts are so many runs of experts / groups; a run counts as its largest c, or with FP4MR_ROUTE_GROUP_SUM2 as the sum of its two largest (c = s then, also without a
- *                bias; a run of one counts as it); only the experts of the top_groups best runs may be chosen
+ *   groups       the experts are so many runs of experts / groups; a run counts as its largest c, or with FP4MR_ROUTE_GROUP_SUM2 as the sum of its two largest; only the experts of the
+ *                top_groups best runs may be chosen.  With that flag and more than one run c = s also without a bias (with one run the flag changes nothing).  Experts that are taken out do not
+ *                count: a run with one expert left counts as that one's c alone, one with none is never chosen.  (A finite bias takes an expert out of the choice, not out of its run's sum.)
  *   the choice   the `top` largest c, in descending order; of equal ones, runs and experts alike, the lower index.  Where a score enters c, c is formed in binary64, else the logits are compared as they are.
  *   weights      scale * s of the chosen, or with FP4MR_ROUTE_RENORM scale * s / max(sum of the chosen s, 2^-60); the bias has no part in them; within 2^-20 of the value or 2^-50 of scale
  * A logit or bias of minus infinity takes an expert out.  A token with fewer than `top` experts left has experts -1, weights 0 and places -1 behind them; one with none (a row of padding, masked whole) has no rows

@@ -72,3 +72,29 @@ def test_infinite_biases(fp4):
         for flags in (0, fp4.ROUTE_SIGMOID, fp4.ROUTE_GROUP_SUM2):
             weights, experts, *_ = check(fp4, z, 5, bias=bias, groups=groups, top_groups=top_groups, flags=flags)
             assert (experts[:, 0] == 7).all() and (experts[:, 1] == 20).all()
+
+
+def test_what_a_run_with_one_expert_left_counts_as(fp4):
+    """The one alone, where minus infinity takes the others out; where a finite bias does, the sum with it."""
+    E, groups = 12, 3
+    z = torch.zeros(2, E, device="cuda")                      # scores of 1/2
+    bias = torch.full((E,), -0.9, device="cuda")              # c = -0.4, sums of two -0.8
+    bias[4:8] = torch.tensor([-0.9, -float("inf"), -float("inf"), -float("inf")])
+    bias[8:] = -1.2                                           # -0.7, -1.4
+    flags = fp4.ROUTE_SIGMOID | fp4.ROUTE_GROUP_SUM2
+    assert (check(fp4, z, 1, bias=bias, groups=groups, top_groups=1, flags=flags)[1] == 4).all()
+    bias[5:8] = -1e30
+    assert (check(fp4, z, 1, bias=bias, groups=groups, top_groups=1, flags=flags)[1] == 0).all()
+    z[1, :8] = -float("inf")
+    assert check(fp4, z, 1, bias=bias, groups=groups, top_groups=1, flags=flags)[1].flatten().tolist() == [0, 8]
+
+
+@pytest.mark.parametrize("biased", [False, True])
+def test_the_sum_of_two_means_nothing_with_one_run(fp4, biased):
+    """Saturated scores are equal, logits are not: without a bias they are compared as they are, whatever the flag."""
+    z = torch.linspace(30.0, 60.0, 16, device="cuda").repeat(3, 1)
+    bias = torch.zeros(16, device="cuda") if biased else None
+    got = [check(fp4, z, 3, bias=bias, flags=fp4.ROUTE_SIGMOID | f) for f in (0, fp4.ROUTE_GROUP_SUM2)]
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    if not biased:
+        assert got[0][1][0].tolist() == [15, 14, 13]
