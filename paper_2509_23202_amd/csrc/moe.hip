@@ -143,10 +143,10 @@ enum { kPacked, kLogit, kScore };
 
 // A score in fp32, from an exponential within two steps, sums in binary64 and a reciprocal, is within 2^-20 of the score: of softmax (x = z - max) s (2^-22 + 2^-22 + 2^-23 + 2^-24) + s 2^-24 sum e^x |x| / sum e^x
 // + 0.37 2^-24, where s times the quotient of sums is less than 2 (0.84 2^-20 in all), of sigmoid s (2^-22 + 2^-24 + 2^-23) + 0.28 2^-24.  With its bias, c is within 2^-20 + 2^-24 |c|.
-// Two that are further apart than both errors, at most 2^-19 + 2^-23 of the larger magnitude, are in the order of their exact values; `apart` asks for twice the second part.  An error grows slower than c, so one that is
-// apart from the next is apart from all behind it; and it is a matter of the two that are compared: an expert that a bias far below the others takes out (-1e9, the type's lowest value) puts no token in
-// doubt (16384 tokens, 8 of 256 experts, one of which is out so: 27 us; with one doubt for all, from the largest bias, every token was routed twice: 53).
-__device__ __forceinline__ bool apart(float larger, float smaller) { return larger - smaller > fmaf(0x1p-22f, fmaxf(larger, -smaller), 0x1p-19f + 0x1p-22f); }
+// Two that are further apart than both errors, at most 2^-19 + 2^-23 of the larger magnitude, are in the order of their exact values (the second-order parts are in the last bit of the factor, and the difference is exact
+// where it is that small).  An error grows slower than c, so one that is apart from the next is apart from all behind it; and it is a matter of the two that are compared: an expert that a bias far below the others takes
+// out (-1e9, the type's lowest value) puts no token in doubt (16384 tokens, 8 of 256 experts, one of which is out so: 27 us; with one doubt for all, from the largest bias, every token was routed twice: 53).
+__device__ __forceinline__ bool apart(float larger, float smaller) { return larger - smaller > fmaf(0x1.00001p-23f, fmaxf(larger, -smaller), 0x1p-19f); }
 
 // The same of sums m of two, f >= s: within 2^-19 + 2^-24 (|f| + |s| + |m|), at most 2^-19 + 2^-23 (|m| + opposed), the lesser magnitude of the two where their signs differ.  What is beyond fp32 counts as its largest
 // number, which the exact sum has passed but for a rounding.
@@ -154,7 +154,7 @@ __device__ __forceinline__ bool sums_apart(float larger, float smaller, float op
 {
     constexpr float MOST = 3.402823466e38f;
     const float l = __builtin_amdgcn_fmed3f(larger, -MOST, MOST), s = __builtin_amdgcn_fmed3f(smaller, -MOST, MOST);
-    return l - s > fmaf(0x1p-21f, fmaxf(l, -s) + opposed, 0x1p-18f + 0x1p-21f);
+    return l - s > fmaf(0x1.00001p-22f, fmaxf(l, -s) + opposed, 0x1p-18f);
 }
 
 // A token's LANES lanes' view of what is the same for all of them.
@@ -184,10 +184,10 @@ struct Token {
     }
 };
 
-// The wave's largest, and 1 at least: what hardly ever counts needs no maximum over the lanes.
+// The wave's largest, and 1/2 at least: what hardly ever counts needs no maximum over the lanes.
 __device__ __forceinline__ float largest_opposed(float opposed)
 {
-    return __any(opposed > 1.0f) ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)lanes_max<64>(__float_as_uint(opposed)))) : 1.0f;
+    return __any(opposed > 0.5f) ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)lanes_max<64>(__float_as_uint(opposed)))) : 0.5f;
 }
 
 // The best top_groups groups, as bits.  key: a function of the expert.  sure: stays so where scores in fp32 leave no doubt.
