@@ -56,9 +56,10 @@ __device__ __forceinline__ void store4(void* out, int64_t at, const v4i& sum, fl
 // ---------------------------------------------------------------- few rows: weights streamed from memory
 // 16 TN columns and 16 TM rows to a tile; a workgroup walks a run of tiles.  Its waves share K, each with a run of blocks; a block's codes go to the wave's own part of LDS by direct-to-LDS loads, D
 // blocks ahead, the next tile's behind this one's, so that what is on its way never runs dry and no wave waits for another but to add up a tile.
-// Bound by memory where columns are many (the experts of 16 tokens, 64 x 4096 x 4096: 6.8 TB/s of weights), else by its start-up and the last tile's sum: 1 x 4096 x 4096 5.6 us (3.0 TB/s), 1 x 10240 x 8192 14.6 (5.7).
-// Four waves and three blocks each cost least at the start; two waves (16 x 32) let three workgroups share a compute unit.  Tiles of 48 and 64 rows, which read the weights once, are level with two of 32 (33 x 4096 x 14336
-// 13.2 us against 15.8, 64 rows 17.5 against 14.7): more of what a compute unit takes in is X then.
+// Bound by memory where columns are many (16 tokens, 4 of 64 experts 4096 x 4096: 28 to 34 experts' weights at 5.5 to 5.7 TB/s), else by its start-up and the last tile's sum: 1 x 4096 x 4096 6.4 us with the weights from
+// memory (2.6 TB/s), 5.6 from the caches, 1 x 10240 x 8192 20.3 (4.1) and 14.8.  Loads go out for sixteen or 32 rows of X whatever there are of them: a third to a half of the load instructions.
+// Four waves and three blocks each cost least at the start; two waves (16 x 32) let three workgroups share a compute unit.  Tiles of 48 and 64 rows, which read the weights once, gain where the caches have the weights
+// (33 x 4096 x 14336 13.2 us against 15.8, 64 rows 17.5 against 14.7) and lose where they come from memory (48 x 16: 33 rows 18.5 against 17.1, 48 rows 21.2 against 19.1): more of what a compute unit takes in is X then.
 template <int TM_, int TN_, int WAVES_, int D_>
 struct Stream {
     static constexpr int TM = TM_, TN = TN_, WAVES = WAVES_, D = D_;
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(C::WAVES * 64) void int8_stream_kernel(Int8Args g, 
             for (int i = 0; i < TN; ++i) read(from + i * 2048, wf[i]);
 #pragma unroll
             for (int t = 0; t < TM; ++t) read(from + (TN + t) * 2048, af[t]);
-            wait_lgkmcnt0();      // (the slot is loaded again by the next issue but D - 2)
+            wait_lgkmcnt0();      // (the slot is loaded again by the very next issue)
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -666,7 +667,9 @@ constexpr int kRows[kKinds] = {16, 16, 32, 32, 64, 128, 128, 128, 256}, kCols[kK
 // them), but no less than what it reads takes from memory at `rate` TB/s: where rows are few the weights, once for the first row of tiles and `again` times for each other one (the caches have part of them), else both
 // operands once, of the `sets` of weights that have rows.  Parts add the writing, reading and launch of their sum.  A product by expert runs longer and is nearer to what memory gives: it has numbers of its own.
 // Measured, each kind and number of parts forced in turn, on 336 products of 1 to 4096 rows with layers from 300 x 9600 to 28672 x 4096 and on 150 drawn ones, weights from memory (450 MB of them in turn): the kind that is
-// chosen takes 1.017 of the best one's time in the mean, 1.017 on 100 others too, at worst 1.26 (16 x 5001 x 2896: 8.1 us on tiles of 16 x 32, 6.4 on 16 x 16); by expert 1.04 on 66 products; the others up to ten times it
+// chosen takes 1.017 of the best one's time in the mean, 1.017 on 100 others too, at worst 1.26 (16 x 5001 x 2896: 8.1 us on tiles of 16 x 32, 6.4 on 16 x 16); by expert 1.04 on 66 products, and 1.05 on 51
+// others, at worst 1.32: 64 experts 4096 x 4096 with 16 to 64 rows each (1024 rows 224 us on tiles of 128 x 64, 188 on 128 x 256; 4096 rows 296 and 223; dealt so unevenly that 29 and 38 experts have rows 124 and 96, 239 and
+// 168).  The others take up to ten times the best one's
 // (1 x 4096 x 4096: 16 x 16 5.9 us, 64 x 64 9.9, 128 x 128 19; 16 x 10240 x 8192: 64 x 64 20.3, 16 x 16 25.6; 128 x 4096 x 14336: 128 x 64 in four parts 23, in one 50; 201 x 10240 x 8192: 128 x 128 27 us, 128 x 64 37,
 // 64 x 64 41, 128 x 256 50; 4096 x 4096 x 4096: 256 x 256 53 us, 128 x 256 63, 128 x 128 65, 64 x 64 100).
 double kind_us(int kind, bool grouped, double rows, double tiles_m, double sets, double N, double K, int64_t blocks, int parts, int cus)

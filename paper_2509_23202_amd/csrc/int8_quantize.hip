@@ -37,7 +37,8 @@ struct QuantArgs {
 };
 
 // A row to T threads, CH times eight values in each one's registers: read once, between its statistics and its codes.  What bounds it is memory: 57344 x 8192 227 us (6.2 TB/s; a large copy reaches 6.4), gated rows of
-// 4096 x 14336 49 us; of few rows the start-up and one compute unit to a row (1 x 4096 2.8 us, 33 gated ones of 14336 4.8).
+// 4096 x 14336 50 us; of few rows the start-up and one compute unit to a row (1 x 4096 2.8 us, 33 gated ones of 14336 4.9).  Narrow rows have one load to a thread, and up to half of the threads none: 16384 rows of 1024
+// columns 12.1 us (4.2 TB/s), 2560 32.2 (3.9), 4096 38.4 (5.2), 4160 41.6 (4.9), 5120 46.7 (5.4), 100000 of 256 27.0 (2.8).
 template <int T, int CH, bool SILU>
 __global__ __launch_bounds__(T) void int8_quantize_kernel(QuantArgs a)
 {
@@ -118,7 +119,7 @@ struct NormArgs {
 };
 
 // The same behind the norm: a row is read once and stays in registers from the sum of its squares to its codes.  The sum is formed in the same order every time: a thread's values, a wave's lanes, the waves.
-// Bound by memory (4095 x 8192 with residual 40 us, 168 MB in and 100 out, part of it from the last-level cache), for one row by its start-up (4096 columns 2.8 us).
+// Bound by memory (4095 x 8192 with residual 43 us on buffers in turn, 134 MB in and 101 out, 5.4 TB/s; 36 where the caches have part of it), for one row by its start-up (4096 columns 2.5 us).
 template <int T, int CH, bool RESIDUAL>
 __global__ __launch_bounds__(T) void int8_rmsnorm_kernel(NormArgs a)
 {

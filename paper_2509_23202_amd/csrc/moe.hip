@@ -10,8 +10,9 @@
 // The chosen pairs (token, place among its choices) are then sorted by expert, stably, so that an expert's rows are in the order of the tokens: counts of each expert for each run of tokens, a
 // sum over the runs in front and the experts in front, and the rank within the run.  No atomic's order reaches a result.
 //
-// What bounds it: for few tokens the launches (1 token of 64 experts 2.8 us), for many the vector unit, some 40 instructions to a token's expert where scores are compared (16384 tokens of 512 experts in groups 51 us, their
-// logits at 6.4 TB/s 5), some 10 where logits are (16384 of 128 7.8 us); the second launch reads all counts in every workgroup (6.5 us).
+// What bounds it: for few tokens the launches (1 token of 64 experts 2.7 us) and a chain of latencies (777 of 256 in groups 8 us, 12 with a token in doubt, the vector unit at work in a sixth of them).  For many the vector
+// unit: it works in 62 % of the cycles where logits are compared (16384 tokens of 128 experts 8.0 us, 154 instructions of a wave to a token), in 77 and 79 % where scores are (of 256 with a bias 21.6 us, 456 of them; of 512
+// in groups 50.6, 1160), while waves wait for half of theirs; reading the logits would take 0.7, 2.6 and 5.3.  The second launch reads all counts in every workgroup (16384 of 128 5.9 us; half of its cycles at work).
 #include "bf16_rows.hpp"
 #include "internal.hpp"
 
@@ -657,7 +658,8 @@ struct CombineArgs {
 
 __device__ __forceinline__ float element(const void* p, int64_t i, bool f32) { return f32 ? static_cast<const float*>(p)[i] : (float)static_cast<const __bf16*>(p)[i]; }
 
-// out[t] = shared[t] + sum_j weight[t,j] y[place[t,j]], in fp32 in the order of the choices.  A choice without a row adds its weight times zero.  Any number of columns, at any element.
+// out[t] = shared[t] + sum_j weight[t,j] y[place[t,j]], in fp32 in the order of the choices.  A choice without a row adds its weight times zero.  Any number of columns, at any element; an element to a thread, whose loads of 2
+// or 4 bytes and whose division bound it: 4095 tokens x 8 rows of 4097 columns 266 us, of 4096 where one of the tensors is off 16 bytes 272 (the kernel below 60).  For odd shapes; a model's rows are whole pieces.
 template <bool Y_F32>
 __global__ __launch_bounds__(256) void moe_combine_any_kernel(CombineArgs a)
 {
@@ -691,7 +693,7 @@ __device__ __forceinline__ void load8(const void* p, int64_t i, bool f32, float 
 }
 
 // The same for rows whose pieces of eight columns are 16-byte aligned, a piece to a thread: the loads of up to eight rows are on their way together.  A token's columns are to `wide` threads, a power of two.
-// Bound by memory: 4095 tokens x 8 rows of 4096 with the shared expert's 58 us (335 MB, 5.8 TB/s; a large copy's 6.4 would be 53); of few tokens by its start-up (5 tokens 3.0 us).
+// Bound by memory: 4095 tokens x 8 rows of 4096 with the shared expert's 58 us (335 MB, 5.8 TB/s; a large copy's 6.4 would be 53), all in fp32 139 (671 MB, 4.8 TB/s); of few tokens by its start-up (5 tokens 2.7 us).
 template <bool Y_F32>
 __global__ __launch_bounds__(256) void moe_combine_kernel(CombineArgs a, int wide)
 {
